@@ -303,6 +303,86 @@ int astra_decode_attention_static(const astra_decode_desc* desc, const void* q, 
                                   const void* codes_k, const void* codes_v, const uint64_t* valid_bits,
                                   const void* codebook_k, const void* codebook_v, void* out, float* lse_out, void* stream);
 
+/* ---- a decoding step of many sequences over a paged cache of 8-bit values --------------------------
+ * Sec. 3.1: after the parallel encoding, decoding goes on at the device that holds the most recent token; a server does
+ * so for many sequences at a time.  Their own tokens' keys and values live in pages of page_size tokens, as e4m3 codes
+ * (1 sign, 4 exponent, 3 mantissa bits, largest value 448, all bits but the sign set: NaN, no infinities) with one scale per page and KV head:
+ *   k_pages, v_pages    [n_pages, H_kv, page_size, dh] bytes;  a value is code * scale
+ *   k_scales, v_scales  [n_pages, H_kv] fp32
+ *   page_table          [n_seqs, table_stride] int32: pages of a sequence in the order of its tokens, the first max_pages
+ *                       entries of a row count.  An entry outside [0, n_pages) is a page that is not there: nothing
+ *                       is written to it and nobody attends to its tokens
+ *   lens                [n_seqs] int32: tokens that a sequence had cached before this step
+ *   first_row           [n_seqs + 1] int32, ascending: the new tokens of sequence s are rows first_row[s] ..
+ *                       first_row[s + 1] - 1 of q, k, v and out; row r is its token lens[s] + r - first_row[s].  Rows that no
+ *                       sequence has are left as they are, and tokens beyond max_pages * page_size are dropped
+ * Both calls of a step take the same descriptor, table, lens and first_row; the caller adds the new tokens to lens
+ * afterwards.  Sequences may share pages that are full; a page that a call writes to belongs to one entry of one sequence.
+ *   q                   rows of H_q * dh elements, q_stride elements apart; k, v: rows of H_kv * dh, k_stride, v_stride
+ * Strides are whole multiples of 16 bytes.  head_dim 64, 128 or 256; page_size 16, 32, 64 or 128; at most 1024 sequences. */
+typedef struct {
+    int32_t dtype;              /* element type of q, k, v, prior_out, out */
+    int32_t n_q_heads, n_kv_heads, head_dim;
+    int32_t page_size, n_pages;
+    int32_t n_seqs;
+    int32_t max_pages;          /* pages that a sequence can have */
+    int32_t table_stride;       /* elements between rows of page_table; 0 means max_pages */
+    int32_t n_tokens;           /* rows of q, k, v and out */
+    int32_t q_stride, k_stride, v_stride;   /* 0 means dense rows */
+    float rope_base;            /* 0: no rotary positions */
+    float scale;                /* of the logits; 0 means 1 / sqrt(head_dim) */
+} astra_cache_desc;
+
+/* Writes the new tokens to the cache.  Keys (and queries) are first turned to their positions: row r of sequence s is at
+ * position lens[s] + r - first_row[s] + pos_shift[s] (pos_shift nullable [n_seqs] int32: the non-local tokens that precede the
+ * device's own), pairs of neighbouring channels as in astra_block_forward.  A block of new values (one page, one head) is stored with
+ *   scale = the smallest power of two with max |value| <= 448 * scale (within 2^-100 .. 2^110), or the scale that the page
+ *           has if it already holds tokens and that is larger;
+ * where the scale of a page that holds tokens grows, those are rounded again to the new one (exact but for values that
+ * become subnormal codes).  Values are rounded once, from fp32 to the nearest code, ties to even; an infinite or NaN value becomes
+ * NaN and does not count for the scale.  Codes of a page beyond its last token are not touched.
+ *   q, q_out            both or neither NULL; same stride; q_out may be q */
+int astra_cache_append(const astra_cache_desc* desc, const int32_t* page_table, const int32_t* lens, const int32_t* first_row,
+                       const int32_t* pos_shift, const void* q, const void* k, const void* v, void* q_out,
+                       uint8_t* k_pages, uint8_t* v_pages, float* k_scales, float* v_scales, void* stream);
+
+/* Attention of the new tokens' queries over the cache, after the step's astra_cache_append:
+ *   out[r, h] = softmax_t( q[r, h] . K[t, h / (H_q/H_kv)] * scale ) V[t],   t = 0 .. token of row r  (its own included)
+ *   prior_out, prior_lse  both or neither NULL: [n_tokens, H_q, dh] and [n_tokens, H_q] fp32, the result of attention over other
+ *                       tokens (astra_decode_attention over the peers' codes: its out and lse_out).  The softmax then covers
+ *                       both sets: out = (e^lse o + e^prior_lse prior_out) / (e^lse + e^prior_lse)
+ *   out                 [n_tokens, H_q, dh] dense; may be prior_out
+ *   lse_out             nullable [n_tokens, H_q] fp32; may be prior_lse.  With nothing to attend to, out = 0 and lse = -inf.
+ *   workspace           astra_cache_attention_workspace_bytes(desc) bytes; 0 for an invalid descriptor
+ * Queries are not turned here.  Results are independent of the run (no atomics). */
+size_t astra_cache_attention_workspace_bytes(const astra_cache_desc* desc);
+
+int astra_cache_attention(const astra_cache_desc* desc, const int32_t* page_table, const int32_t* lens, const int32_t* first_row,
+                          const void* q, const uint8_t* k_pages, const uint8_t* v_pages, const float* k_scales,
+                          const float* v_scales, const void* prior_out, const float* prior_lse, void* out, float* lse_out,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* Products of a few tokens with weights of 4 bits (Sec. 4.4 combines the method with weights quantised after training):
+ *   y[t, n] = bias[n] + sum_k x[t, k] * scales[n, k / group] * (code[n, k] - zeros[n, k / group])
+ *   x        [n_tokens, in_features], rows x_stride elements apart
+ *   codes    [out_features, in_features / 2] bytes: column 2i in the lower four bits of byte i, column 2i + 1 in the upper
+ *   scales   [out_features, in_features / group] in the element type
+ *   zeros    nullable [out_features, in_features / group] bytes, 0 .. 15 (their lower four bits count); NULL means 8
+ *   bias     nullable [out_features] in the element type
+ *   y        [n_tokens, out_features], fp32 or bf16 (y_dtype)
+ * group 32, 64 or 128, a divisor of in_features.  Sums are kept in fp32.  The kernel reads the weights once for every 64
+ * tokens: many tokens are served correctly, but are the business of the layer's own products. */
+typedef struct {
+    int32_t dtype;              /* element type of x, scales, bias */
+    int32_t y_dtype;
+    int32_t in_features, out_features;
+    int32_t group;
+    int32_t x_stride;           /* 0 means in_features; a whole multiple of 16 bytes */
+} astra_w4_desc;
+
+int astra_w4_linear(const astra_w4_desc* desc, const void* x, int64_t n_tokens, const uint8_t* codes, const void* scales,
+                    const uint8_t* zeros, const void* bias, void* y, void* stream);
+
 /* ---- one whole Transformer block on one device -------------------------------------------------
  * Sec. 3.1: per block, a device quantises its local token embeddings, exchanges indices, attends with
  * the mixed-precision layer and then runs the position-wise MLP locally, without communication.  The

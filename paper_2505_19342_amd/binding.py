@@ -21,6 +21,7 @@ EXPORTS = ("astra_vq_prepare", "astra_vq_encode", "astra_vq_encode_workspace_byt
            "astra_layer_kv_workspace_bytes", "astra_layer_forward_kv",
            "astra_decode_attention_workspace_bytes", "astra_decode_attention",
            "astra_decode_attention_static_max_bytes", "astra_decode_attention_static",
+           "astra_cache_append", "astra_cache_attention_workspace_bytes", "astra_cache_attention", "astra_w4_linear",
            "astra_codebook_stats_workspace_bytes", "astra_codebook_stats", "astra_codebook_update", "astra_navq_forward",
            "astra_probe_mfma_bf16", "astra_status_string", "astra_version")
 ASTRA_NORM_LAYER, ASTRA_NORM_RMS = 0, 1
@@ -56,6 +57,16 @@ class LayerKvDesc(ctypes.Structure):
 class DecodeDesc(ctypes.Structure):
     _fields_ = [("vq", VqDesc), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("n_local", ctypes.c_int32), ("n_nonlocal", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class CacheDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "n_q_heads", "n_kv_heads", "head_dim", "page_size", "n_pages", "n_seqs", "max_pages",
+                                              "table_stride", "n_tokens", "q_stride", "k_stride", "v_stride")]
+    _fields_ += [("rope_base", ctypes.c_float), ("scale", ctypes.c_float)]
+
+
+class W4Desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "y_dtype", "in_features", "out_features", "group", "x_stride")]
 
 
 class BlockDesc(ctypes.Structure):
@@ -125,6 +136,14 @@ def load(build_if_missing: bool = True):
     lib.astra_decode_attention_static_max_bytes.restype = ctypes.c_size_t
     lib.astra_decode_attention_static.argtypes = [ctypes.POINTER(DecodeDesc)] + [vp] * 11
     lib.astra_decode_attention_static.restype = ctypes.c_int
+    lib.astra_cache_append.argtypes = [ctypes.POINTER(CacheDesc)] + [vp] * 13
+    lib.astra_cache_append.restype = ctypes.c_int
+    lib.astra_cache_attention_workspace_bytes.argtypes = [ctypes.POINTER(CacheDesc)]
+    lib.astra_cache_attention_workspace_bytes.restype = ctypes.c_size_t
+    lib.astra_cache_attention.argtypes = [ctypes.POINTER(CacheDesc)] + [vp] * 13 + [ctypes.c_size_t, vp]
+    lib.astra_cache_attention.restype = ctypes.c_int
+    lib.astra_w4_linear.argtypes = [ctypes.POINTER(W4Desc), vp, i64, vp, vp, vp, vp, vp, vp]
+    lib.astra_w4_linear.restype = ctypes.c_int
     lib.astra_codebook_stats_workspace_bytes.argtypes = [ctypes.POINTER(VqDesc), i64]
     lib.astra_codebook_stats_workspace_bytes.restype = ctypes.c_size_t
     lib.astra_codebook_stats.argtypes = [ctypes.POINTER(VqDesc), vp, vp, i64, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
@@ -311,6 +330,130 @@ def astra_decode_attention_static(desc: DecodeDesc, q, k_cache, v_cache, codes_k
                                                 _ptr(lse_out), _stream()), "astra_decode_attention_static")
 
 
+def _array(t, dtypes, n: int, device: int, what: str, strided: bool = False):
+    """Device address of an array of at least n elements on the current device; strided: a view whose rows may lie apart."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.get_device() != device:
+        raise AstraError(f"{what}: a tensor on the current device required")
+    if t.dtype not in dtypes:
+        raise AstraError(f"{what}: element type {t.dtype}, one of {dtypes} required")
+    if t.numel() < n:
+        raise AstraError(f"{what}: {t.numel()} elements, {n} required")
+    if not strided and not t.is_contiguous():
+        raise AstraError(f"{what}: contiguous tensor required")
+    return t.data_ptr()
+
+
+_types = None
+
+
+def _dtypes():
+    """element types by ASTRA_F32 / ASTRA_BF16, whole numbers, codes, fp32, and the function that tells the current device"""
+    global _types
+    if _types is None:
+        import torch
+        _types = (((torch.float32,), (torch.bfloat16,)), (torch.int32,), (torch.uint8, getattr(torch, "float8_e4m3fn", torch.uint8)), (torch.float32,),
+                  torch._C._cuda_getDevice)
+    return _types
+
+
+def _rows(t, n: int, row: int, stride: int, types, device: int, what: str):
+    """Address of n rows of `row` elements that lie `stride` (0: row) elements apart: a contiguous tensor that holds them, or a view whose first
+    stride is that and whose rows are dense."""
+    if t is None:
+        return None
+    a = _array(t, types, n * row, device, what, strided=True)
+    if stride in (0, row):
+        if not t.is_contiguous():
+            raise AstraError(f"{what}: dense rows required; give the row stride in the descriptor")
+        return a
+    if t.is_contiguous():
+        fits = t.numel() >= (n - 1) * stride + row
+    else:
+        fits = t.dim() >= 2 and t.shape[0] >= n and t.stride(0) == stride and t[0].is_contiguous()
+    if not fits:
+        raise AstraError(f"{what}: rows of {row} elements, {stride} apart, required")
+    return a
+
+
+def _cache_arrays(d: CacheDesc, page_table, lens, first_row, k_pages, v_pages, k_scales, v_scales, ints, codes, f32, dev):
+    stride = d.table_stride or d.max_pages
+    blocks = d.n_pages * d.n_kv_heads
+    values = blocks * d.page_size * d.head_dim
+    return (_array(page_table, ints, max(d.n_seqs - 1, 0) * stride + (d.max_pages if d.n_seqs > 0 else 0), dev, "page_table"), _array(lens, ints, d.n_seqs, dev, "lens"),
+            _array(first_row, ints, d.n_seqs + 1, dev, "first_row"), _array(k_pages, codes, values, dev, "k_pages"),
+            _array(v_pages, codes, values, dev, "v_pages"), _array(k_scales, f32, blocks, dev, "k_scales"), _array(v_scales, f32, blocks, dev, "v_scales"))
+
+
+def astra_cache_append(desc: CacheDesc, page_table, lens, first_row, pos_shift, q, k, v, q_out, k_pages, v_pages, k_scales, v_scales):
+    """page_table, lens, first_row, pos_shift: int32; k_pages, v_pages: uint8 or float8_e4m3fn.  q, k, v, q_out may be views of wider rows
+    (desc.q_stride, k_stride, v_stride)."""
+    elem, ints, codes, f32, device = _dtypes()
+    dev, dh = device(), desc.head_dim
+    x = elem[desc.dtype] if desc.dtype in (0, 1) else ()
+    table, le, first, kp, vp, ks, vs = _cache_arrays(desc, page_table, lens, first_row, k_pages, v_pages, k_scales, v_scales, ints, codes, f32, dev)
+    _check(load().astra_cache_append(
+        ctypes.byref(desc), table, le, first, _array(pos_shift, ints, desc.n_seqs, dev, "pos_shift"),
+        _rows(q, desc.n_tokens, desc.n_q_heads * dh, desc.q_stride, x, dev, "q"), _rows(k, desc.n_tokens, desc.n_kv_heads * dh, desc.k_stride, x, dev, "k"),
+        _rows(v, desc.n_tokens, desc.n_kv_heads * dh, desc.v_stride, x, dev, "v"), _rows(q_out, desc.n_tokens, desc.n_q_heads * dh, desc.q_stride, x, dev, "q_out"),
+        kp, vp, ks, vs, _stream()), "astra_cache_append")
+
+
+def astra_cache_attention_workspace_bytes(desc: CacheDesc) -> int:
+    return int(load().astra_cache_attention_workspace_bytes(ctypes.byref(desc)))
+
+
+def astra_cache_attention(desc: CacheDesc, page_table, lens, first_row, q, k_pages, v_pages, k_scales, v_scales, prior_out, prior_lse, out,
+                          lse_out, workspace):
+    """Arguments as for astra_cache_append; prior_out, prior_lse and lse_out may be None."""
+    elem, ints, codes, f32, device = _dtypes()
+    dev, n = device(), desc.n_tokens * desc.n_q_heads
+    x = elem[desc.dtype] if desc.dtype in (0, 1) else ()
+    table, le, first, kp, vp, ks, vs = _cache_arrays(desc, page_table, lens, first_row, k_pages, v_pages, k_scales, v_scales, ints, codes, f32, dev)
+    _check(load().astra_cache_attention(
+        ctypes.byref(desc), table, le, first, _rows(q, desc.n_tokens, desc.n_q_heads * desc.head_dim, desc.q_stride, x, dev, "q"), kp, vp, ks, vs,
+        _array(prior_out, x, n * desc.head_dim, dev, "prior_out"), _array(prior_lse, f32, n, dev, "prior_lse"), _array(out, x, n * desc.head_dim, dev, "out"),
+        _array(lse_out, f32, n, dev, "lse_out"), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream()), "astra_cache_attention")
+
+
+def astra_w4_linear(desc: W4Desc, x, n_tokens: int, codes, scales, zeros, bias, y):
+    """codes, zeros: uint8 (see quantize_w4); zeros and bias may be None."""
+    elem, _, _, _, device = _dtypes()
+    dev, n_in, n_out = device(), desc.in_features, desc.out_features
+    xt, yt = (elem[i] if i in (0, 1) else () for i in (desc.dtype, desc.y_dtype))
+    groups = n_out * (n_in // desc.group) if desc.group > 0 else 0
+    u8 = _types[2][:1]
+    _check(load().astra_w4_linear(
+        ctypes.byref(desc), _rows(x, n_tokens, n_in, desc.x_stride, xt, dev, "x"), n_tokens, _array(codes, u8, n_out * n_in // 2, dev, "codes"),
+        _array(scales, xt, groups, dev, "scales"), _array(zeros, u8, groups, dev, "zeros"), _array(bias, xt, n_out, dev, "bias"),
+        _array(y, yt, n_tokens * n_out, dev, "y"), _stream()), "astra_w4_linear")
+
+
+def quantize_w4(w, group: int, dtype: str = "bf16", zeros: bool = False):
+    """Host helper: weights [out, in] (numpy) as astra_w4_linear takes them: codes [out, in / 2] uint8, scales [out, in / group] fp32 (values of the
+    element type `dtype`), zeros [out, in / group] uint8 or None.  A group's codes are the nearest of 16 evenly spaced values: -8 .. 7 times its scale, the
+    largest magnitude being 7, or with `zeros` from a smallest to a largest value that have zero between them."""
+    import numpy as np
+    from .workloads import round_to_bf16
+    w = np.asarray(w, dtype=np.float32)
+    n_out, n_in = w.shape
+    if group not in (32, 64, 128) or n_in % group:
+        raise AstraError("groups of 32, 64 or 128 columns that divide the width required")
+    g = w.reshape(n_out, n_in // group, group)
+    if zeros:
+        lo, hi = np.minimum(g.min(2), 0.0), np.maximum(g.max(2), 0.0)
+        scale = (hi - lo) / np.float32(15.0)
+    else:
+        scale = np.abs(g).max(2) / np.float32(7.0)
+    scale = np.where(scale > 0, scale, 1.0).astype(np.float32)
+    if dtype == "bf16":
+        scale = np.maximum(round_to_bf16(scale), np.float32(2.0 ** -126))
+    zero = np.clip(np.rint(-lo / scale), 0, 15) if zeros else np.full(scale.shape, 8.0, np.float32)
+    q = np.clip(np.rint(g / scale[..., None]) + zero[..., None], 0, 15).astype(np.uint8).reshape(n_out, n_in)
+    return q[:, 0::2] | (q[:, 1::2] << 4), scale, zero.astype(np.uint8) if zeros else None
+
+
 def astra_codebook_stats_workspace_bytes(desc: VqDesc, n_tokens: int) -> int:
     return int(load().astra_codebook_stats_workspace_bytes(ctypes.byref(desc), n_tokens))
 
@@ -429,3 +572,14 @@ def attn_desc(dtype: str, n_q_heads: int, n_kv_heads: int, head_dim: int, n_cls:
 
 def block_desc(layer: LayerDesc, norm_kind: str, mlp_kind: str, d_ff: int, eps: float, rope_base: float = 0.0) -> BlockDesc:
     return BlockDesc(layer, NORM_KINDS[norm_kind], MLP_KINDS[mlp_kind], d_ff, eps, rope_base)
+
+
+def cache_desc(dtype: str, n_q_heads: int, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, n_seqs: int, max_pages: int, n_tokens: int, *,
+               table_stride: int = 0, q_stride: int = 0, k_stride: int = 0, v_stride: int = 0, rope_base: float = 0.0, scale: float = 0.0) -> CacheDesc:
+    return CacheDesc(ASTRA_BF16 if dtype == "bf16" else ASTRA_F32, n_q_heads, n_kv_heads, head_dim, page_size, n_pages, n_seqs, max_pages, table_stride,
+                     n_tokens, q_stride, k_stride, v_stride, rope_base, scale)
+
+
+def w4_desc(dtype: str, in_features: int, out_features: int, group: int, y_dtype: str | None = None, x_stride: int = 0) -> W4Desc:
+    kinds = {"f32": ASTRA_F32, "bf16": ASTRA_BF16}
+    return W4Desc(kinds[dtype], kinds[y_dtype or dtype], in_features, out_features, group, x_stride)

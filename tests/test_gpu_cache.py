@@ -1,0 +1,319 @@
+"""GPU: the paged cache of 8-bit values (astra_cache_append, astra_cache_attention) against the 64-bit oracle (oracle/serving.py).
+Bars come from the arithmetic (serving_util.attention_bar and beside the comparisons)."""
+import numpy as np
+import pytest
+
+from oracle import serving as sv
+from serving_util import Step, attend, check_attention, dev
+from paper_2505_19342_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- append
+def append(st, base=0.0, shift=None, with_q=True, fused=False, in_place=False):
+    import torch
+    from gpu_util import to_dev, to_host
+    more = {}
+    q, k, v = (to_dev(a, st.dtype) for a in (st.q, st.k, st.v))
+    if fused:                                # rows of one projection of q, k and v
+        row = torch.cat([a.flatten(1) for a in (q, k, v)], 1)
+        cut = (st.hq * st.dh, st.hkv * st.dh, st.hkv * st.dh)
+        q, k, v = row.split(cut, 1)
+        more = {n + "_stride": row.shape[1] for n in "qkv"}
+    q_out = q if in_place else torch.empty_strided(q.shape, q.stride(), dtype=q.dtype, device=q.device).fill_(7.0)
+    pools = [dev(a) for a in (*st.pages, *st.scales)]
+    B.astra_cache_append(st.desc(rope_base=base, **more), dev(st.table), dev(st.lens), dev(st.first), None if shift is None else dev(np.asarray(shift, np.int32)),
+                         q if with_q else None, k, v, q_out if with_q else None, *pools)
+    torch.cuda.synchronize()
+    got_q = to_host(q_out.contiguous()).reshape(st.q.shape) if with_q else None
+    return got_q, [p.cpu().numpy() for p in pools]
+
+
+def check_append(st, base=0.0, shift=None, **how):
+    got_q, (kp, vp, ks, vs) = append(st, base, shift, **how)
+    want_q, wkp, wvp, wks, wvs, exact = sv.cache_append(st.table, st.lens, st.first, shift, st.q, st.k, st.v, *st.pages, *st.scales, base=base)
+    n = st.first[-1]
+    np.testing.assert_array_equal(ks, wks.astype(np.float32))
+    np.testing.assert_array_equal(vs, wvs.astype(np.float32))
+    one = lambda a: np.where(a & 127 == 127, 127, a)                              # the type has a NaN of either sign
+    kp, wkp = one(kp), one(wkp)
+    np.testing.assert_array_equal(one(vp), one(wvp))                              # not turned: the same operations on both sides
+    # keys: a turned value is off by 2^-22 of its pair at most (cosine and sine within 2^-23 each, two products), so a code may fall to the other side of a
+    # border between two that is nearer than that
+    val = sv.e4m3_values()
+    for p, h, o, c in zip(*np.nonzero(kp != wkp)):
+        x = exact[0][p, h, o] / wks[p, h]                                         # KeyError: a row that had to stay as it was
+        pair = np.abs(x.reshape(-1, 2)).sum(1)[c // 2]
+        border = (val[kp[p, h, o, c]] + val[wkp[p, h, o, c]]) / 2
+        assert abs(x[c] - border) <= 2.0 ** -22 * pair, (p, h, o, c)
+    if got_q is not None:
+        pair = np.repeat(np.abs(st.q).reshape(*st.q.shape[:2], -1, 2).sum(3), 2, 2)
+        bar = 2.0 ** -22 * pair + (2.0 ** -8 if st.dtype == "bf16" else 2.0 ** -24) * np.abs(want_q)
+        assert np.all(np.abs(got_q - want_q)[:n] <= bar[:n])
+        assert np.array_equal(got_q[n:], st.q[n:]) if how.get("in_place") else np.all(got_q[n:] == 7.0)
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+@pytest.mark.parametrize("dtype, heads", [("bf16", (8, 2, 128)), ("f32", (3, 3, 64)), ("bf16", (6, 2, 256)), ("f32", (5, 1, 128))])
+def test_append(dtype, heads, page):
+    """One token, some, and a prompt, into empty, partly filled and full pages; sequences without new tokens and rows behind the last one."""
+    check_append(Step(dtype, *heads, page, [0, 1, page - 1, page, 3 * page + 5, 40, 2, 7], [1, 1, 1, 1, 1, 0, 1, 1], seed=page, behind=3), 500000.0)
+    check_append(Step(dtype, *heads, page, [0, 2 * page - 3, 5, 0], [3 * page + 1, 5, 0, page], seed=page + 1, behind=2), 10000.0)
+
+
+def test_append_of_a_long_prompt_far_ahead():
+    check_append(Step("bf16", 4, 2, 128, 64, [100], [1100], seed=1), 500000.0, shift=[98304], with_q=True)
+
+
+@pytest.mark.parametrize("how", [dict(fused=True), dict(fused=True, in_place=True), dict(with_q=False), dict(in_place=True)])
+def test_append_from_views_and_in_place(how):
+    check_append(Step("bf16", 4, 2, 128, 32, [30, 0, 9], [1, 40, 2], seed=2, behind=1), 10000.0, shift=[5, 0, 1000], **how)
+    check_append(Step("f32", 4, 1, 64, 16, [3], [1], seed=3), 0.0, **how)
+
+
+@pytest.mark.parametrize("std, spread", [(1e-3, (0, 3)), (300.0, (-30, -20)), (1e-36, (-100, -99)), (1e37, (-8, -5))])
+def test_append_to_scales_far_from_what_comes(std, spread):
+    """Scales that stay, that grow by far (codes of earlier tokens become subnormal or zero), and the ends of the range."""
+    check_append(Step("f32", 2, 2, 64, 32, [5, 31, 0], [3, 20, 2], seed=4, std=std, spread=spread))
+
+
+def test_append_of_zeros_infinities_and_nan():
+    for dtype in ("f32", "bf16"):
+        st = Step(dtype, 2, 2, 64, 16, [4, 0, 0, 0], [3, 2, 1, 18], seed=5)
+        st.k[0, 0, 3], st.k[1, 1, :], st.v[2, 0, 5], st.v[3], st.k[5], st.v[4, 1, 63] = np.inf, np.nan, -np.inf, 0.0, 0.0, np.nan
+        check_append(st)                     # not turned: infinities stay where they are
+    st.k[:] = 1.0
+    check_append(st, 10000.0)
+
+
+def test_append_leaves_what_it_is_not_given():
+    """Pages that are not there, lengths at and beyond the capacity, below zero, and rows that no sequence has."""
+    st = Step("bf16", 2, 1, 64, 16, [14, 30, 0, 5], [4, 3, 20, 2], seed=6)
+    st.table[0, 1], st.table[2, 0], st.table[3, 0] = -1, st.n_pages, 2 ** 31 - 1
+    check_append(st, 10000.0)
+    st = Step("bf16", 2, 1, 64, 16, [14, 30], [4, 3], seed=6)
+    _, before = None, [a.copy() for a in (*st.pages, *st.scales)]
+    for lens in ([10 ** 9, 2 ** 31 - 1], [16 * st.table.shape[1]] * 2):
+        st.lens = np.array(lens, np.int32)
+        for a, b in zip(append(st, 10000.0)[1], before):
+            np.testing.assert_array_equal(a, b)
+
+
+def test_append_in_many_steps_is_the_prompt():
+    """Tokens one by one: the scale of a block only grows, so its codes are those of the prompt up to the rounding of values that became subnormal."""
+    st = Step("bf16", 2, 2, 128, 32, [0], [45], seed=7)
+    _, (kp, vp, ks, vs) = append(st, 10000.0)
+    one = Step("bf16", 2, 2, 128, 32, [0], [45], seed=7)
+    q, k, v, n = one.q, one.k, one.v, 0
+    for take in (1, 1, 5, 1, 24, 1, 3, 9):
+        one.lens, one.first, one.n = np.array([n], np.int32), np.array([0, take], np.int32), take
+        one.q, one.k, one.v = q[n:n + take], k[n:n + take], v[n:n + take]
+        _, (p0, p1, s0, s1) = append(one, 10000.0)
+        one.pages, one.scales, n = [p0, p1], [s0, s1], n + take
+    used = st.table[0, :2]
+    np.testing.assert_array_equal(ks[used], one.scales[0][used])
+    np.testing.assert_array_equal(vs[used], one.scales[1][used])
+    val = sv.e4m3_values()
+    for a, b in ((kp, one.pages[0]), (vp, one.pages[1])):
+        a, b = a.transpose(0, 2, 1, 3)[used].reshape(64, -1)[:45], b.transpose(0, 2, 1, 3)[used].reshape(64, -1)[:45]
+        assert np.all(np.abs(val[a] - val[b]) <= 2.0 ** -9)                       # a step of the subnormal codes
+
+
+# ---- attention
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+@pytest.mark.parametrize("dtype, heads", [("bf16", (8, 2, 128)), ("bf16", (3, 3, 64)), ("bf16", (20, 1, 64)), ("bf16", (4, 4, 256)), ("f32", (6, 2, 64)), ("f32", (8, 1, 128)),
+                                          ("f32", (2, 1, 256))])
+def test_attention_of_single_tokens(dtype, heads, page):
+    check_attention(Step(dtype, *heads, page, [0, 1, 15, 16, 17, 31, 32, 200, 0, 333], [1, 1, 1, 1, 1, 1, 1, 1, 0, 1], seed=page, behind=2).fill())
+
+
+@pytest.mark.parametrize("dtype, heads, page", [("bf16", (8, 2, 128), 64), ("bf16", (3, 3, 64), 16), ("bf16", (5, 1, 128), 32), ("f32", (6, 2, 64), 32), ("bf16", (4, 2, 256), 128)])
+def test_attention_of_several_tokens(dtype, heads, page):
+    check_attention(Step(dtype, *heads, page, [0, 50, 7, 100], [37, 3, 0, 70], seed=page, behind=1).fill())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_of_long_and_uneven_contexts(dtype):
+    check_attention(Step(dtype, 8, 2, 128, 64, [5000, 0, 1], [1, 1, 1], seed=8).fill())
+    check_attention(Step(dtype, 4, 4, 64, 16, [3001], [2], seed=9).fill(), scale=0.3)
+
+
+def test_attention_joined_to_a_prior_result():
+    for dtype in ("bf16", "f32"):
+        st = Step(dtype, 8, 2, 128, 32, [70, 0, 900, 3], [1, 2, 1, 1], seed=10, behind=1).fill()
+        prior = st.rnd(st.rng.standard_normal(st.q.shape).astype(np.float32))
+        lse = (st.rng.standard_normal((st.n, st.hq)) + 6).astype(np.float32)
+        lse[0, :3], prior[0, 0] = -np.inf, np.nan                       # a prior over nothing counts for nothing, whatever it holds
+        lse[1] = 60.0
+        check_attention(st, prior, lse)
+        st.table[2] = -1                                                # nothing of its own: the prior alone
+        check_attention(st, prior, lse)
+
+
+def test_attention_leaves_pages_out():
+    st = Step("bf16", 4, 2, 128, 16, [100, 40, 60], [1, 3, 20], seed=11).fill()
+    st.table[0, 2], st.table[0, 6], st.table[1], st.table[2, 0] = -5, st.n_pages, -1, 2 ** 31 - 1
+    check_attention(st)
+
+
+def test_attention_with_lengths_that_nothing_backs():
+    """Lengths beyond the table are those of the table, below zero they are zero; rows out of range are nobody's."""
+    st = Step("bf16", 2, 1, 64, 16, [31, 31], [1, 1], seed=12).fill()  # all 32 tokens of two pages (a 31 st alone would leave a row of NaN to attend to)
+    ref, _ = attend(st)
+    st.table = np.ascontiguousarray(st.table[:, :2])
+    st.lens = np.array([10 ** 9, -7], np.int32)
+    out, lse = attend(st)
+    assert np.isfinite(out).all() and np.isfinite(lse).all()
+    st.lens = np.array([31, 31], np.int32)
+    st.first = np.array([0, 1, 2 ** 31 - 1], np.int32)
+    np.testing.assert_array_equal(attend(st)[0], ref)
+    st.first = np.array([-9, 1, 2], np.int32)
+    assert np.isfinite(attend(st)[0]).all()
+
+
+def test_nan_values_reach_only_the_rows_that_see_them():
+    for dtype in ("bf16", "f32"):
+        st = Step(dtype, 4, 2, 128, 16, [40], [9], seed=13).fill()
+        p = st.table[0, 45 // 16]
+        st.pages[1][p, 1, 45 % 16, 70] = 0xff                           # a new token's value is NaN in one channel
+        st.pages[0][st.table[0, 47 // 16], 0, 47 % 16, 3] = 0x7f        # and a later one's key
+        ref, ref_lse = sv.cache_attention(st.table, st.lens, st.first, st.q, *st.pages, *st.scales)
+        out, lse = attend(st)
+        nan = np.zeros_like(ref, bool)
+        nan[5:, 2:, 70] = True
+        nan[7:, :2] = True
+        assert np.array_equal(np.isnan(out), nan) and np.array_equal(np.isnan(lse), np.isnan(ref_lse))
+        assert np.array_equal(np.isnan(ref), nan)
+        from serving_util import attention_bar
+        bar, _ = attention_bar(st, np.nan_to_num(ref), 0.0)
+        assert np.all((np.abs(out - ref) <= bar)[~nan])
+
+
+def test_attention_of_one_row_at_a_time_gives_the_same_sums_again():
+    """A second call gives the same bits, whatever the workspace held."""
+    st = Step("bf16", 8, 2, 128, 64, [4000, 17, 900], [1, 4, 1], seed=14).fill()
+    a, b = attend(st), attend(st)
+    assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1])
+
+
+# ---- the step as it is used
+def run_step(st, s, w, base=10000.0):
+    """Append and attend on torch's current stream; returns the arrays that the step writes."""
+    import torch
+    B.astra_cache_append(s["desc"], s["table"], s["lens"], s["first"], None, s["q"], s["k"], s["v"], s["q_out"], *s["pools"])
+    B.astra_cache_attention(s["desc"], s["table"], s["lens"], s["first"], s["q_out"], *s["pools"], None, None, s["out"], s["lse"], w)
+
+
+def state(st, base=10000.0):
+    import torch
+    from gpu_util import empty_like_dtype, to_dev
+    d = st.desc(rope_base=base)
+    s = dict(desc=d, table=dev(st.table), lens=dev(st.lens), first=dev(st.first), pools=[dev(a) for a in (*st.pages, *st.scales)])
+    s.update({n: to_dev(getattr(st, n), st.dtype) for n in "qkv"}, q_out=empty_like_dtype(st.q.shape, st.dtype), out=empty_like_dtype(st.q.shape, st.dtype),
+             lse=torch.empty((st.n, st.hq), device="cuda:0"))
+    return s, torch.full((B.astra_cache_attention_workspace_bytes(d),), 255, dtype=torch.uint8, device="cuda:0")
+
+
+def test_steps_captured_into_a_graph():
+    """A decoding loop: the graph appends, attends and counts the tokens up; every replay against the same steps made eagerly, with other work between."""
+    import torch
+    st = Step("bf16", 8, 2, 128, 16, [60, 0, 15], [1, 1, 1], seed=15)
+    st.table[:, 4:] = -1
+    more = np.arange(st.n_pages, st.n_pages + 6, dtype=np.int32).reshape(3, 2)          # pages to grow into
+    held = [4, 1, 1]
+    table = np.full((3, 8), -1, np.int32)
+    for i in range(3):
+        table[i, :held[i]] = st.table[i, :held[i]]
+        table[i, held[i]:held[i] + 2] = more[i]
+    st.table, st.n_pages = table, st.n_pages + 6
+    st.pages = [np.concatenate((p, np.full((6, *p.shape[1:]), 127, np.uint8))) for p in st.pages]
+    st.scales = [np.concatenate((p, np.full((6, p.shape[1]), np.nan, np.float32))) for p in st.scales]
+    e, we = state(st)
+    g, wg = state(st)
+    keep = {n: g[n].clone() for n in ("lens",)}, [p.clone() for p in g["pools"]]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run_step(st, g, wg)                                                              # once before the capture
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run_step(st, g, wg)
+        g["lens"].add_(1)
+    g["lens"].copy_(keep[0]["lens"])
+    for a, b in zip(g["pools"], keep[1]):
+        a.copy_(b)
+    for i in range(20):
+        for n in "qkv":
+            x = torch.randn(e[n].shape, device="cuda:0").to(e[n].dtype)
+            e[n].copy_(x)
+            g[n].copy_(x)
+        run_step(st, e, we)
+        e["lens"].add_(1)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(e["out"], g["out"]) and torch.equal(e["lse"], g["lse"]), i
+        for a, b in zip(e["pools"], g["pools"]):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), i
+        assert torch.isfinite(g["out"].float()).all()
+
+
+def test_steps_on_two_streams_at_once():
+    import torch
+    parts = [Step("bf16", 8, 2, 128, 64, lens, [1] * len(lens), seed=16 + i) for i, lens in enumerate(([2000, 3, 900], [10, 3000], [700] * 9))]
+    want = []
+    for st in parts:
+        s, w = state(st)
+        run_step(st, s, w)
+        torch.cuda.synchronize()
+        want.append(s["out"].clone())
+    both = [state(st) for st in parts]
+    streams = [torch.cuda.Stream() for _ in parts]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for st, (s, w), q in zip(parts, both, streams):
+            with torch.cuda.stream(q):
+                run_step(st, s, w)
+    torch.cuda.synchronize()
+    for (s, _), x in zip(both, want):
+        assert torch.equal(s["out"], x)
+
+
+def test_a_devices_step_joins_the_peers_codes():
+    """Astra's step at the device that holds the latest token: attention over the peers' codes (astra_decode_attention without local rows), then over the own tokens in
+    the paged cache, joined: the softmax over both, by the oracle of either set."""
+    import torch
+    import oracle
+    from gpu_util import codes_to_dev, empty_like_dtype, to_dev, to_host
+    for dtype, bar in (("bf16", 1e-2), ("f32", 1e-5)):
+        st = Step(dtype, 8, 2, 128, 64, [130], [1], seed=20).fill()
+        G, K, peers = 8, 64, 300
+        cb = [st.rnd((st.rng.standard_normal((G, K, 2 * 128 // G)) * 1.2).astype(np.float32)) for _ in range(2)]
+        codes = [st.rng.integers(0, K, (peers, G)).astype(np.int32) for _ in range(2)]
+        d = B.DecodeDesc(B.vq_desc(dtype, 256, G, K), 8, 2, 128, 0, peers, 0.0)
+        prior, plse = empty_like_dtype((8, 128), dtype), torch.empty(8, device="cuda:0")
+        ws = torch.empty(max(B.astra_decode_attention_workspace_bytes(d), 256), dtype=torch.uint8, device="cuda:0")
+        B.astra_decode_attention(d, to_dev(st.q[0], dtype), None, None, codes_to_dev(codes[0], K), codes_to_dev(codes[1], K), None, to_dev(cb[0], dtype),
+                                 to_dev(cb[1], dtype), prior, plse, ws)
+        s, w = state(st, 0.0)
+        B.astra_cache_attention(s["desc"], s["table"], s["lens"], s["first"], s["q"], *s["pools"], prior, plse, prior, plse, w)           # joined in place
+        torch.cuda.synchronize()
+        none = np.zeros((0, 2, 128), np.float32)
+        p, pl = oracle.decode_attention(st.q[0], none, none, codes[0], codes[1], *cb, return_lse=True)
+        ref, ref_lse = sv.cache_attention(st.table, st.lens, st.first, st.q, *st.pages, *st.scales, prior=p[None], prior_lse=pl[None])
+        # the prior comes rounded to the element type (the bars of the decode step's own tests, and this call's)
+        from serving_util import attention_bar
+        assert np.all(np.abs(to_host(prior) - ref[0]) <= attention_bar(st, ref[0], 0.0)[0] + bar)
+        assert np.all(np.abs(plse.cpu().numpy() - ref_lse[0]) <= 2e-4)
+
+
+def test_tensors_of_another_device_are_refused():
+    import torch
+    st = Step("bf16", 2, 1, 64, 16, [3], [1], seed=21).fill()
+    s, w = state(st)
+    for n in ("table", "q", "lens"):
+        with pytest.raises(B.AstraError):
+            B.astra_cache_attention(s["desc"], *[s[m].cpu() if m == n else s[m] for m in ("table", "lens", "first", "q")], *s["pools"], None, None, s["out"], None, w)
+    with pytest.raises(B.AstraError, match="workspace"):
+        B.astra_cache_attention(s["desc"], s["table"], s["lens"], s["first"], s["q"], *s["pools"], None, None, s["out"], None, w[:128])

@@ -30,6 +30,7 @@ __device__ __forceinline__ V ld_global(gbytes at) { return *reinterpret_cast<con
 
 __device__ __forceinline__ f32x4 mfma_16x16x32(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
+struct CaJoin;
 struct CacheAttnParams {
     CacheStep c;
     const void* q;
@@ -43,10 +44,10 @@ struct CacheAttnParams {
     float* lse;
     int32_t q_stride;
     float scale;
-    // scratch, see CacheAttnScratch
+    // scratch, see CacheAttnPlan
     float* part_o;
     float* part_ml;
-    int4* joins;
+    CaJoin* joins;
 };
 
 template <bool HIGH>
@@ -61,22 +62,17 @@ __device__ __forceinline__ bf16x8 eight_codes(uint32_t lo, uint32_t hi) {
     w.w = two_codes<true>(hi);
     return __builtin_bit_cast(bf16x8, w);
 }
-// the value of the lane 32 or 16 away
-template <int X>
-__device__ __forceinline__ float xor_rows(float v) {
-    const uint32_t w = __float_as_uint(v);
-    if constexpr (X == 32) {
-        const auto r = __builtin_amdgcn_permlane32_swap(w, w, false, false);        // lower halves of both, upper halves of both
-        return __uint_as_float(lane_id() & 32 ? r[0] : r[1]);
-    } else {
-        const auto r = __builtin_amdgcn_permlane16_swap(w, w, false, false);
-        return __uint_as_float(lane_id() & 16 ? r[0] : r[1]);
-    }
+// largest of the four lanes of a column (16 apart)
+__device__ __forceinline__ float column_max(float v) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);        // lower halves of both, upper halves of both
+    const float w = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(w), __float_as_uint(w), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 // 1 in each byte of w that is NaN (all seven bits below the sign set)
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return (((w & 0x7f7f7f7fu) + 0x01010101u) >> 7) & 0x01010101u; }
 
-// What a wavefront knows of its query rows: a block of 16 rows (new token, head) of one sequence and KV head
+// What a wavefront knows of its query rows: a block of 16 or 32 rows (new token, head) of one sequence and KV head
 struct RowBlock {
     int seq, kv_head;
     int len, n_new, from;        // cached tokens, new tokens, first row of the sequence
@@ -84,7 +80,8 @@ struct RowBlock {
     int least, all;              // tokens that the block's first row and its last one attend to
 };
 
-template <int DH, typename T>
+// NT: groups of 16 query rows
+template <int DH, typename T, int NT>
 struct CacheWalk {
     static constexpr int KJ = DH / 64;         // 16-byte pieces of a key row per lane
     static constexpr int KC = DH / 32;         // contraction steps of a score
@@ -109,40 +106,53 @@ struct CacheWalk {
         __device__ __forceinline__ int64_t block(const CacheStep& c, int hf, int kv_head) const { return (int64_t)(there(c, hf) ? id[hf] : 0) * c.Hkv + kv_head; }
     };
 
-    bf16x8 q[QP][KC];
-    f32x4 acc[VCH];
-    float m, l;
-    int sees;                                  // tokens that this lane's row attends to
+    bf16x8 q[NT][QP][KC];
+    f32x4 acc[NT][VCH];
+    float m[NT], l[NT];
+    int sees[NT];                              // tokens that this lane's rows attend to
 
     __device__ __forceinline__ void start(const CacheAttnParams& p, const RowBlock& b) {
         const int lane = lane_id(), col = lane & 15, g = lane >> 4;
         const int share = p.c.Hq / p.c.Hkv;
-        const int row = min(b.row0 + col, b.n_rows - 1), token = row / share, head = b.kv_head * share + row - token * share;
-        sees = min(b.len + token + 1, p.c.capacity());
-        const gbytes at = (gbytes)p.q + ((int64_t)(b.from + token) * p.q_stride + head * DH + 16 * g) * (int64_t)sizeof(T);
 #pragma unroll
-        for (int kc = 0; kc < KC; ++kc) {
-            const gbytes a = at + (64 * (kc >> 1) + 8 * (kc & 1)) * (int)sizeof(T);
-            if constexpr (!F32) {
-                q[0][kc] = __builtin_bit_cast(bf16x8, ld_global<u32x4>(a));
-            } else {
-                const f32x4 x0 = ld_global<f32x4>(a), x1 = ld_global<f32x4>(a + 16);
+        for (int n = 0; n < NT; ++n) {
+            const int row = min(b.row0 + 16 * n + col, b.n_rows - 1), token = row / share, head = b.kv_head * share + row - token * share;
+            sees[n] = min(b.len + token + 1, p.c.capacity());
+            const gbytes at = (gbytes)p.q + ((int64_t)(b.from + token) * p.q_stride + head * DH + 16 * g) * (int64_t)sizeof(T);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float x = e < 4 ? x0[e & 3] : x1[e & 3];
+            for (int kc = 0; kc < KC; ++kc) {
+                const gbytes a = at + (64 * (kc >> 1) + 8 * (kc & 1)) * (int)sizeof(T);
+                if constexpr (!F32) {
+                    q[n][0][kc] = __builtin_bit_cast(bf16x8, ld_global<u32x4>(a));
+                } else {
+                    const f32x4 x0 = ld_global<f32x4>(a), x1 = ld_global<f32x4>(a + 16);
 #pragma unroll
-                    for (int i = 0; i < QP; ++i) {             // every difference is exact
-                        const float part = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
-                        q[i][kc][e] = (__bf16)part;
-                        x -= part;
+                    for (int e = 0; e < 8; ++e) {
+                        float x = e < 4 ? x0[e & 3] : x1[e & 3];
+#pragma unroll
+                        for (int i = 0; i < QP; ++i) {             // every difference is exact
+                            const float part = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+                            q[n][i][kc][e] = (__bf16)part;
+                            x -= part;
+                        }
                     }
                 }
             }
-        }
 #pragma unroll
-        for (int c = 0; c < VCH; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-        m = -INFINITY;
-        l = 0.f;
+            for (int c = 0; c < VCH; ++c) acc[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+            m[n] = -INFINITY;
+            l[n] = 0.f;
+        }
+    }
+
+    __device__ __forceinline__ void nothing() {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int c = 0; c < VCH; ++c) acc[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+            m[n] = -INFINITY;
+            l[n] = 0.f;
+        }
     }
 
     // token of score / value element e inside a tile
@@ -188,32 +198,37 @@ struct CacheWalk {
     }
 
     // scores of a tile in base-2 units, not yet masked
-    __device__ __forceinline__ void score(const CacheAttnParams& p, const Keys& x, float (&s)[8]) const {
+    __device__ __forceinline__ void score(const CacheAttnParams& p, const Keys& x, float (&s)[NT][8]) const {
         const float sl2 = p.scale * kLog2e;
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
-            f32x4 d = {0.f, 0.f, 0.f, 0.f};
+            f32x4 d[NT] = {};
 #pragma unroll
             for (int kc = 0; kc < KC; ++kc) {
                 const u32x4& w = x.k[hf][kc >> 1];
                 const bf16x8 kf = kc & 1 ? eight_codes(w.z, w.w) : eight_codes(w.x, w.y);
 #pragma unroll
-                for (int i = 0; i < QP; ++i) d = mfma_16x16x32(kf, q[i][kc], d);
+                for (int i = 0; i < QP; ++i)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) d[n] = mfma_16x16x32(kf, q[n][i][kc], d[n]);
             }
             const float f = sl2 * x.scale[hf];
 #pragma unroll
-            for (int v = 0; v < 4; ++v) s[4 * hf + v] = d[v] * f;
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) s[n][4 * hf + v] = d[n][v] * f;
         }
     }
 
     // scores and values of a tile into the running sums
-    __device__ __forceinline__ void absorb(const CacheAttnParams& p, const RowBlock& b, int t, const Pages& pg, float (&s)[8], Values& x) {
+    __device__ __forceinline__ void absorb(const CacheAttnParams& p, const RowBlock& b, int t, const Pages& pg, float (&s)[NT][8], Values& x) {
         const int g = lane_id() >> 4;
         const bool there[2] = {pg.there(p.c, 0), pg.there(p.c, 1)};
         if (t * kCaTile + kCaTile > b.least || !there[0] || !there[1]) {        // of the whole wavefront
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                s[e] = there[e >> 2] && t * kCaTile + tok(e, g) < sees ? s[e] : -INFINITY;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) s[n][e] = there[e >> 2] && t * kCaTile + tok(e, g) < sees[n] ? s[n][e] : -INFINITY;
                 if (!there[e >> 2]) x.v[e] = Piece{};
             }
 #pragma unroll
@@ -226,30 +241,32 @@ struct CacheWalk {
                 for (int d = 0; d < VCH / 4; ++d) bad |= nan_bytes(word(x.v[e], d));
             if (__builtin_expect(__builtin_amdgcn_ballot_w64(bad != 0) != 0, 0)) careful(t, x);
         }
-        float mx = s[0];
+        u32x4 part[NT][PP];
 #pragma unroll
-        for (int e = 1; e < 8; ++e) mx = fmaxf(mx, s[e]);
-        mx = fmaxf(mx, xor_rows<32>(mx));                    // the four lanes of a column share one reference
-        mx = fmaxf(mx, xor_rows<16>(mx));
-        const float m_new = fmaxf(m, mx), ref = m_new == -INFINITY ? 0.f : m_new;
-        const float alpha = __builtin_amdgcn_exp2f(m - ref);
-        l *= alpha;
+        for (int n = 0; n < NT; ++n) {
+            float mx = s[n][0];
 #pragma unroll
-        for (int c = 0; c < VCH; ++c) acc[c] *= alpha;
-        m = m_new;
-        u32x4 part[PP];
+            for (int e = 1; e < 8; ++e) mx = fmaxf(mx, s[n][e]);
+            // (sums are rescaled with every tile: under a branch for the tiles that raise the reference by much they take a second set of registers)
+            const float m_new = fmaxf(m[n], column_max(mx)), ref = m_new == -INFINITY ? 0.f : m_new;
+            const float alpha = __builtin_amdgcn_exp2f(m[n] - ref);
+            l[n] *= alpha;
 #pragma unroll
-        for (int e = 0; e < 8; e += 2) {
-            float a = __builtin_amdgcn_exp2f(s[e] - ref), c = __builtin_amdgcn_exp2f(s[e + 1] - ref);
-            l += a;
-            l += c;
-            a *= x.scale[e >> 2];
-            c *= x.scale[e >> 2];
+            for (int c = 0; c < VCH; ++c) acc[n][c] *= alpha;
+            m[n] = m_new;
 #pragma unroll
-            for (int i = 0; i < PP; ++i) {                    // the upper halves of both; what is left of them is exact
-                part[i][e >> 1] = __builtin_amdgcn_perm(__float_as_uint(c), __float_as_uint(a), 0x07060302u);
-                a -= __uint_as_float(__float_as_uint(a) & 0xffff0000u);
-                c -= __uint_as_float(__float_as_uint(c) & 0xffff0000u);
+            for (int e = 0; e < 8; e += 2) {
+                float a = __builtin_amdgcn_exp2f(s[n][e] - ref), c = __builtin_amdgcn_exp2f(s[n][e + 1] - ref);
+                l[n] += a;
+                l[n] += c;
+                a *= x.scale[e >> 2];
+                c *= x.scale[e >> 2];
+#pragma unroll
+                for (int i = 0; i < PP; ++i) {                    // the upper halves of both; what is left of them is exact
+                    part[n][i][e >> 1] = __builtin_amdgcn_perm(__float_as_uint(c), __float_as_uint(a), 0x07060302u);
+                    a -= __uint_as_float(__float_as_uint(a) & 0xffff0000u);
+                    c -= __uint_as_float(__float_as_uint(c) & 0xffff0000u);
+                }
             }
         }
 #pragma unroll
@@ -263,10 +280,12 @@ struct CacheWalk {
                 hi[e >> 1] = two_codes<true>(w);
             }
 #pragma unroll
-            for (int i = 0; i < PP; ++i) {
-                acc[2 * c2] = mfma_16x16x32(__builtin_bit_cast(bf16x8, lo), __builtin_bit_cast(bf16x8, part[i]), acc[2 * c2]);
-                acc[2 * c2 + 1] = mfma_16x16x32(__builtin_bit_cast(bf16x8, hi), __builtin_bit_cast(bf16x8, part[i]), acc[2 * c2 + 1]);
-            }
+            for (int i = 0; i < PP; ++i)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    acc[n][2 * c2] = mfma_16x16x32(__builtin_bit_cast(bf16x8, lo), __builtin_bit_cast(bf16x8, part[n][i]), acc[n][2 * c2]);
+                    acc[n][2 * c2 + 1] = mfma_16x16x32(__builtin_bit_cast(bf16x8, hi), __builtin_bit_cast(bf16x8, part[n][i]), acc[n][2 * c2 + 1]);
+                }
         }
     }
 
@@ -274,28 +293,31 @@ struct CacheWalk {
     // Products of ones (NaN here, token seen there) tell which sums become NaN; the NaN values themselves become zeros.
     __device__ __forceinline__ void careful(int t, Values& x) {
         const int g = lane_id() >> 4;
-        u32x4 seen;
 #pragma unroll
-        for (int e = 0; e < 8; e += 2) {
-            const int token = t * kCaTile + tok(e, g);
-            seen[e >> 1] = (token < sees ? 0x3f80u : 0u) | (token + 1 < sees ? 0x3f800000u : 0u);          // values that are not there are zeros
-        }
-#pragma unroll
-        for (int c2 = 0; c2 < VCH / 2; ++c2) {
-            u32x4 lo, hi;
+        for (int n = 0; n < NT; ++n) {
+            u32x4 seen;
 #pragma unroll
             for (int e = 0; e < 8; e += 2) {
-                const uint32_t w = 0x38u * nan_bytes(__builtin_amdgcn_perm(word(x.v[e + 1], c2 >> 1), word(x.v[e], c2 >> 1), c2 & 1 ? 0x07030602u : 0x05010400u));
-                lo[e >> 1] = two_codes<false>(w);
-                hi[e >> 1] = two_codes<true>(w);
+                const int token = t * kCaTile + tok(e, g);
+                seen[e >> 1] = (token < sees[n] ? 0x3f80u : 0u) | (token + 1 < sees[n] ? 0x3f800000u : 0u);          // values that are not there are zeros
             }
-            const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-            const f32x4 a = mfma_16x16x32(__builtin_bit_cast(bf16x8, lo), __builtin_bit_cast(bf16x8, seen), zero);
-            const f32x4 b = mfma_16x16x32(__builtin_bit_cast(bf16x8, hi), __builtin_bit_cast(bf16x8, seen), zero);
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                acc[2 * c2][v] = a[v] > 0.f ? NAN : acc[2 * c2][v];
-                acc[2 * c2 + 1][v] = b[v] > 0.f ? NAN : acc[2 * c2 + 1][v];
+            for (int c2 = 0; c2 < VCH / 2; ++c2) {
+                u32x4 lo, hi;
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const uint32_t w = 0x38u * nan_bytes(__builtin_amdgcn_perm(word(x.v[e + 1], c2 >> 1), word(x.v[e], c2 >> 1), c2 & 1 ? 0x07030602u : 0x05010400u));
+                    lo[e >> 1] = two_codes<false>(w);
+                    hi[e >> 1] = two_codes<true>(w);
+                }
+                const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+                const f32x4 a = mfma_16x16x32(__builtin_bit_cast(bf16x8, lo), __builtin_bit_cast(bf16x8, seen), zero);
+                const f32x4 b = mfma_16x16x32(__builtin_bit_cast(bf16x8, hi), __builtin_bit_cast(bf16x8, seen), zero);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    acc[n][2 * c2][v] = a[v] > 0.f ? NAN : acc[n][2 * c2][v];
+                    acc[n][2 * c2 + 1][v] = b[v] > 0.f ? NAN : acc[n][2 * c2 + 1][v];
+                }
             }
         }
 #pragma unroll
@@ -307,41 +329,47 @@ struct CacheWalk {
         }
     }
 
-    // of a column, once all tiles are in
+    // of the columns, once all tiles are in
     __device__ __forceinline__ void finish_sum() {
-        l += __shfl_xor(l, 16);
-        l += __shfl_xor(l, 32);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            l[n] += __shfl_xor(l[n], 16);
+            l[n] += __shfl_xor(l[n], 32);
+        }
     }
 };
 
 // ---- the work of a launch, dealt out --------------------------------------------------------------
-// A unit is a tile of 32 tokens for one row block.  The units of all row blocks (sequence by sequence, head by head, block by block of 16 rows, the tiles of a
+// A unit is a tile of 32 tokens for one row block.  The units of all row blocks (sequence by sequence, head by head, block by block of rows, the tiles of a
 // block in order) are cut into equal shares, one per workgroup: ragged batches keep every workgroup busy equally long, and one long context is
-// walked by all of them.  Only the device knows the lengths, so every workgroup adds them up itself.  The four wavefronts take the tiles
+// walked by all of them.  Only the device knows the lengths, so every workgroup adds them up itself.  The wavefronts take the tiles
 // of a share in turn and are joined in LDS.  Where a share ends inside a row block, the unnormalised sums go to the scratch array:
 // a workgroup has at most two such pieces, one that ends a row block begun by others (slot 2w) and one that begins one (slot 2w + 1).
 // The workgroup that begins a block notes how many pieces there are, and a second launch joins them in order.
-constexpr int kCaWaves = 4, kCaThreads = kCaWaves * kWave;
-constexpr int kCaMinShare = 8;        // tiles, two per wavefront
-constexpr int kCaRows = 16;
-
-// what their registers leave room for
-template <int DH, typename T>
-constexpr int kCaWgsPerCu = (DH == 64 ? 4 : DH == 128 ? 3 : 2) - (sizeof(T) == 4 ? 1 : 0);
+// Where sequences cannot be long (CUT = false), a row block is one unit, the workgroups have more wavefronts and there is no second launch.
+constexpr int kCaMinShare = 8;        // tiles
 constexpr int kCaCus = 256;
+constexpr int kCaMaxTiles = 64;       // of a sequence that is not cut
 
-__device__ __forceinline__ int n_blocks(int n_rows) { return (n_rows + kCaRows - 1) / kCaRows; }
+// how many wavefronts a workgroup has and how many workgroups the registers of a unit leave room for
+template <int DH, typename T, int NT, bool CUT>
+struct CaShape {
+    static constexpr int per_simd = DH == 256 ? (sizeof(T) == 4 ? 1 : 2) : DH == 128 ? (sizeof(T) == 4 || NT > 1 ? 2 : 3) : (sizeof(T) == 4 || NT > 1 ? 3 : 4);
+    static constexpr int waves = CUT ? 4 : 4 * (per_simd > 3 ? 3 : per_simd), threads = waves * kWave;
+    static constexpr int wgs_per_cu = CUT ? per_simd : 1;
+};
+
+// what joins the pieces of a row block
+struct CaJoin {
+    int32_t pieces, row0, n_rows, kv_head, from, pad[3];
+};
 
 struct SequencePlan {
-    int len, from, n_new, tiles, blocks;
-    __device__ __forceinline__ SequencePlan(const CacheStep& c, int s) {
-        len = cache_len(c, s);
-        from = cache_row(c, s);
-        n_new = max(cache_row(c, s + 1) - from, 0);
-        tiles = (int)((min((int64_t)len + n_new, (int64_t)c.capacity()) + kCaTile - 1) / kCaTile);
-        blocks = n_blocks(n_new * (c.Hq / c.Hkv));
-    }
-    __device__ __forceinline__ int64_t units(const CacheStep& c) const { return (int64_t)tiles * blocks * c.Hkv; }
+    int len, from, n_new;
+    __device__ __forceinline__ SequencePlan(int l, int f, int n) : len(l), from(f), n_new(n) {}
+    __device__ __forceinline__ SequencePlan(const CacheStep& c, int s) : len(cache_len(c, s)), from(cache_row(c, s)), n_new(max(cache_row(c, s + 1) - from, 0)) {}
+    __device__ __forceinline__ uint32_t tiles(const CacheStep& c) const { return (uint32_t)(min(len + n_new, c.capacity()) + kCaTile - 1) / kCaTile; }
+    __device__ __forceinline__ uint32_t blocks(const CacheStep& c, int rows) const { return (uint32_t)(n_new * (c.Hq / c.Hkv) + rows - 1) / (uint32_t)rows; }
 };
 
 template <typename T>
@@ -355,7 +383,8 @@ template <typename T>
 struct RowResult {
     int64_t at;
     float wo, wp, lse;
-    __device__ __forceinline__ RowResult(const CacheAttnParams& p, int64_t row_head, float m, float l) : at(row_head), wp(0.f) {
+    __device__ __forceinline__ RowResult(const CacheAttnParams& p, bool wanted, int64_t row_head, float m, float l) : at(row_head), wo(0.f), wp(0.f), lse(0.f) {
+        if (!wanted) return;
         wo = l != 0.f ? 1.f / l : 0.f;
         lse = l != 0.f ? kLn2 * m + logf(l) : -INFINITY;
         if (p.prior_lse) {
@@ -386,282 +415,329 @@ struct RowResult {
     }
 };
 
-template <int DH, typename T>
-__global__ __launch_bounds__(kCaThreads, (kCaWgsPerCu<DH, T>)) void cache_attn_kernel(const CacheAttnParams p) {
-    using Walk = CacheWalk<DH, T>;
-    constexpr int PASS = 4;                                       // channels per thread and pass when the wavefronts are joined
-    constexpr int STRIDE = 16 * PASS + 4;
-    __shared__ int64_t before[kCacheMaxSeqs + 1];                 // units before a sequence
-    __shared__ int64_t wave_sum[kCaWaves];
-    __shared__ float ml[kCaWaves][kCaRows][2];
-    __shared__ __align__(16) float sums[kCaWaves][kCaRows][STRIDE];
+template <int DH, typename T, int NT, bool CUT>
+__global__ __launch_bounds__((CaShape<DH, T, NT, CUT>::threads), (CaShape<DH, T, NT, CUT>::wgs_per_cu)) void cache_attn_kernel(const CacheAttnParams p) {
+    using Walk = CacheWalk<DH, T, NT>;
+    constexpr int WAVES = CaShape<DH, T, NT, CUT>::waves, THREADS = WAVES * kWave, ROWS = 16 * NT;
+    constexpr int PASS = 4, STRIDE = 16 * PASS + 4;               // channels per thread and pass when the wavefronts are joined
+    __shared__ uint32_t before[kCacheMaxSeqs + 1];                // units before a sequence, where there are more than 64
+    __shared__ float ml[WAVES][ROWS][2];
+    __shared__ __align__(16) float sums[WAVES][16][STRIDE];
+    // the arguments arrive together; each use asking for its own is another trip to them
+    asm volatile("" ::"s"(p.c.table), "s"(p.c.lens), "s"(p.c.first), "s"(p.q), "s"(p.k_pages), "s"(p.v_pages), "s"(p.k_scales), "s"(p.v_scales), "s"(p.c.n_seqs),
+                 "s"(p.c.n_tokens), "s"(p.c.max_pages), "s"(p.c.table_stride), "s"(p.c.n_pages), "s"(p.c.page_shift), "s"(p.c.Hq), "s"(p.c.Hkv), "s"(p.q_stride),
+                 "s"(p.scale));
     const CacheStep& c = p.c;
     const int tid = threadIdx.x, lane = lane_id(), col = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int share_h = c.Hq / c.Hkv;
 
-    {
-        constexpr int PER = kCacheMaxSeqs / kCaThreads;
-        int64_t mine[PER], sum = 0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int s = tid * PER + i;
-            mine[i] = sum;
-            if (s < c.n_seqs) sum += SequencePlan(c, s).units(c);
-        }
-        int64_t scan = sum;
+    auto units = [&](const SequencePlan& sp) __attribute__((always_inline)) { return (CUT ? sp.tiles(c) : 1u) * sp.blocks(c, ROWS) * (uint32_t)c.Hkv; };
+    auto scan = [&](uint32_t x) __attribute__((always_inline)) {       // sum of the lanes up to this one
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
-            const int64_t up = __shfl_up(scan, o);
-            if (lane >= o) scan += up;
+            const uint32_t up = __shfl_up(x, o);
+            if (lane >= o) x += up;
         }
-        if (lane == 63) wave_sum[wave] = scan;
+        return x;
+    };
+    // up to 64 sequences: a lane has one of them
+    SequencePlan lane_plan(0, 0, 0);
+    uint32_t lane_before = 0, all;
+    const bool few = c.n_seqs <= 64;
+    if (few) {
+        if (lane < c.n_seqs) lane_plan = SequencePlan(c, lane);
+        const uint32_t mine = lane < c.n_seqs ? units(lane_plan) : 0u, upto = scan(mine);
+        lane_before = upto - mine;
+        all = __builtin_amdgcn_readlane(upto, 63);
+    } else {
+        if (wave == 0) {
+            uint32_t base = 0;
+            for (int s0 = 0; s0 < c.n_seqs; s0 += 64) {
+                const int s = s0 + lane;
+                const uint32_t mine = s < c.n_seqs ? units(SequencePlan(c, s)) : 0u, upto = scan(mine);
+                if (s < c.n_seqs) before[s] = base + upto - mine;
+                base += __builtin_amdgcn_readlane(upto, 63);
+            }
+            if (lane == 0) before[c.n_seqs] = base;
+        }
         __syncthreads();
-        int64_t base = scan - sum;
-        for (int w = 0; w < wave; ++w) base += wave_sum[w];
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (tid * PER + i <= c.n_seqs) before[tid * PER + i] = base + mine[i];
-        if (tid == kCaThreads - 1 && c.n_seqs == kCacheMaxSeqs) before[kCacheMaxSeqs] = base + sum;
-        __syncthreads();
+        all = before[c.n_seqs];
     }
-    const int64_t all = before[c.n_seqs];
-    const int64_t share = max((all + gridDim.x - 1) / (int64_t)gridDim.x, (int64_t)kCaMinShare);
-    int64_t u = (int64_t)blockIdx.x * share;
-    const int64_t end = min(u + share, all);
-    int4 join = {0, 0, 0, 0};
+    const uint32_t share = CUT ? max((all + gridDim.x - 1) / gridDim.x, (uint32_t)kCaMinShare) : 1u;
+    uint32_t u = blockIdx.x < (all + share - 1) / share ? blockIdx.x * share : all;
+    const uint32_t end = all - u < share ? all : u + share;
+    CaJoin join = {};
 
     while (u < end) {
-        int lo = 0, n = c.n_seqs;                // the last sequence that begins at or before u; those without units are behind it
-        while (n > 0) {
-            const int half = n >> 1;
-            if (before[lo + half] <= u) {
-                lo += half + 1;
-                n -= half + 1;
-            } else {
-                n = half;
+        // the last sequence that begins at or before u; those without units are before it
+        int s;
+        uint32_t in;
+        SequencePlan sp(0, 0, 0);
+        if (few) {
+            s = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64(lane < c.n_seqs && lane_before <= u));
+            in = u - (uint32_t)__builtin_amdgcn_readlane(lane_before, s);
+            sp = SequencePlan(__builtin_amdgcn_readlane(lane_plan.len, s), __builtin_amdgcn_readlane(lane_plan.from, s), __builtin_amdgcn_readlane(lane_plan.n_new, s));
+        } else {
+            int lo = 0, n = c.n_seqs;
+            while (n > 0) {
+                const int half = n >> 1;
+                if (before[lo + half] <= u) {
+                    lo += half + 1;
+                    n -= half + 1;
+                } else {
+                    n = half;
+                }
             }
+            s = __builtin_amdgcn_readfirstlane(lo - 1);
+            in = u - before[s];
+            sp = SequencePlan(c, s);
         }
-        const int s = __builtin_amdgcn_readfirstlane(lo - 1);
-        const SequencePlan sp(c, s);
-        const int64_t in = u - before[s], row = in / sp.tiles;
-        const int tile0 = __builtin_amdgcn_readfirstlane((int)(in - row * sp.tiles));
-        const int count = __builtin_amdgcn_readfirstlane((int)min((int64_t)(sp.tiles - tile0), end - u));
+        const uint32_t all_tiles = sp.tiles(c), blocks = sp.blocks(c, ROWS), tiles = CUT ? all_tiles : 1u;
+        const uint32_t row = in / tiles;
+        const int tile0 = __builtin_amdgcn_readfirstlane((int)(in - row * tiles));
+        const int count = __builtin_amdgcn_readfirstlane((int)min(tiles - tile0, end - u));
         RowBlock b;
         b.seq = s;
-        b.kv_head = __builtin_amdgcn_readfirstlane((int)(row / sp.blocks));
+        b.kv_head = __builtin_amdgcn_readfirstlane((int)(row / blocks));
         b.len = __builtin_amdgcn_readfirstlane(sp.len);
         b.n_new = __builtin_amdgcn_readfirstlane(sp.n_new);
         b.from = __builtin_amdgcn_readfirstlane(sp.from);
         b.n_rows = b.n_new * share_h;
-        b.row0 = __builtin_amdgcn_readfirstlane((int)(row % sp.blocks)) * kCaRows;
-        b.least = (int)min((int64_t)b.len + b.row0 / share_h + 1, (int64_t)c.capacity());
-        b.all = (int)min((int64_t)b.len + min(b.row0 + kCaRows - 1, b.n_rows - 1) / share_h + 1, (int64_t)c.capacity());
+        b.row0 = __builtin_amdgcn_readfirstlane((int)(row % blocks)) * ROWS;
+        b.least = min(b.len + b.row0 / share_h + 1, c.capacity());
+        b.all = min(b.len + min(b.row0 + ROWS - 1, b.n_rows - 1) / share_h + 1, c.capacity());
 
         Walk w;
-        w.start(p, b);
-        {
-            // The next tile's keys are asked for as soon as this one's have become scores, its values once this one's are in the sums, the numbers of
-            // its pages a tile earlier; beyond the last tile it is asked for again, so that there is one body and no wait covers more than it is for.
-            const int stop = min(tile0 + count, (b.all + kCaTile - 1) / kCaTile);
-            int t = tile0 + wave;
-            if (t < stop) {
-                typename Walk::Keys k;
-                typename Walk::Values v;
-                typename Walk::Pages now = Walk::pages(p, b, t);
-                Walk::load(p, b, t, now, k);
-                Walk::load(p, b, t, now, v);
-                typename Walk::Pages next = Walk::pages(p, b, min(t + kCaWaves, stop - 1));
-                for (;;) {
-                    const int then = min(t + kCaWaves, stop - 1);
-                    float s[8];
-                    w.score(p, k, s);
-                    Walk::load(p, b, then, next, k);
-                    w.absorb(p, b, t, now, s, v);
-                    Walk::load(p, b, then, next, v);
-                    t += kCaWaves;
-                    if (t >= stop) break;
-                    now = next;
-                    next = Walk::pages(p, b, min(t + kCaWaves, stop - 1));
-                }
+        // The next tile's keys are asked for as soon as this one's have become scores, its values once this one's are in the sums, the numbers of
+        // its pages a tile earlier; beyond the last tile it is asked for again, so that there is one body and no wait covers more than it is for.
+        const int stop = min(CUT ? tile0 + count : (int)all_tiles, (b.all + kCaTile - 1) / kCaTile);
+        int t = tile0 + wave;
+        if (t < stop) {
+            typename Walk::Keys k;
+            typename Walk::Values v;
+            typename Walk::Pages now = Walk::pages(p, b, t);
+            typename Walk::Pages next = Walk::pages(p, b, min(t + WAVES, stop - 1));
+            w.start(p, b);
+            Walk::load(p, b, t, now, k);
+            Walk::load(p, b, t, now, v);
+            for (;;) {
+                const int then = min(t + WAVES, stop - 1);
+                float s[NT][8];
+                w.score(p, k, s);
+                Walk::load(p, b, then, next, k);
+                w.absorb(p, b, t, now, s, v);
+                Walk::load(p, b, then, next, v);
+                t += WAVES;
+                if (t >= stop) break;
+                now = next;
+                next = Walk::pages(p, b, min(t + WAVES, stop - 1));
             }
+        } else {
+            w.nothing();
         }
         w.finish_sum();
 
         // the wavefronts' sums, under the largest of their references
-        if (g == 0) {
-            ml[wave][col][0] = w.m;
-            ml[wave][col][1] = w.l;
-        }
+        if (g == 0)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                ml[wave][16 * n + col][0] = w.m[n];
+                ml[wave][16 * n + col][1] = w.l[n];
+            }
         __syncthreads();
-        float m = ml[0][col][0];
-#pragma unroll
-        for (int i = 1; i < kCaWaves; ++i) m = fmaxf(m, ml[i][col][0]);
-        const float f = w.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(w.m - m);
-        // from here on a thread has a row and a 16th of its channels
-        const int r = tid >> 4, piece = tid & 15;
-        float mr = ml[0][r][0], lr = 0.f;
-#pragma unroll
-        for (int i = 1; i < kCaWaves; ++i) mr = fmaxf(mr, ml[i][r][0]);
-#pragma unroll
-        for (int i = 0; i < kCaWaves; ++i) lr += ml[i][r][0] == -INFINITY ? 0.f : ml[i][r][1] * __builtin_amdgcn_exp2f(ml[i][r][0] - mr);
-        const int my_row = b.row0 + r;
-        const bool mine = my_row < b.n_rows, whole = count == sp.tiles;
-        const int token = mine ? my_row / share_h : 0, head = b.kv_head * share_h + my_row - token * share_h;
-        const int64_t at = (int64_t)(b.from + token) * c.Hq + head;
+        const bool whole = !CUT || count == (int)tiles;
         const int64_t slot = 2 * (int64_t)blockIdx.x + (tile0 == 0 ? 1 : 0);
-        auto channels = [&](int pass, float(&o)[PASS]) __attribute__((always_inline)) {
-            __syncthreads();                     // the pass before has been read
 #pragma unroll
-            for (int v = 0; v < 4; ++v)
+        for (int n = 0; n < NT; ++n) {
+            float m = ml[0][16 * n + col][0];
 #pragma unroll
-                for (int e = 0; e < PASS; e += 4)
-                    *reinterpret_cast<f32x4*>(&sums[wave][col][(4 * g + v) * PASS + e]) =
-                        f32x4{w.acc[pass * PASS + e][v] * f, w.acc[pass * PASS + e + 1][v] * f, w.acc[pass * PASS + e + 2][v] * f, w.acc[pass * PASS + e + 3][v] * f};
-            __syncthreads();
+            for (int i = 1; i < WAVES; ++i) m = fmaxf(m, ml[i][16 * n + col][0]);
+            const float f = w.m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(w.m[n] - m);
+            // from here on a thread of the first 256 has a row and a 16th of its channels
+            const int r = (tid >> 4) & 15, piece = tid & 15;
+            float mr = ml[0][16 * n + r][0], lr = 0.f;
 #pragma unroll
-            for (int e = 0; e < PASS; e += 4) {
-                f32x4 t = {0.f, 0.f, 0.f, 0.f};
+            for (int i = 1; i < WAVES; ++i) mr = fmaxf(mr, ml[i][16 * n + r][0]);
 #pragma unroll
-                for (int i = 0; i < kCaWaves; ++i) t += *reinterpret_cast<const f32x4*>(&sums[i][r][piece * PASS + e]);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) o[e + k] = t[k];
-            }
-        };
-        if (whole) {
-            float o[Walk::VCH / PASS][PASS];
-#pragma unroll
-            for (int pass = 0; pass < Walk::VCH / PASS; ++pass) channels(pass, o[pass]);
-            if (mine) {
-                const RowResult<T> res(p, at, mr, lr);
-#pragma unroll
-                for (int pass = 0; pass < Walk::VCH / PASS; ++pass) res.store(p, DH, Walk::VCH * piece + pass * PASS, o[pass]);
-                if (p.lse && piece == 0) p.lse[at] = res.lse;
-            }
-        } else {
+            for (int i = 0; i < WAVES; ++i) lr += ml[i][16 * n + r][0] == -INFINITY ? 0.f : ml[i][16 * n + r][1] * __builtin_amdgcn_exp2f(ml[i][16 * n + r][0] - mr);
+            const int my_row = b.row0 + 16 * n + r;
+            const bool mine = tid < 256 && my_row < b.n_rows;
+            const int token = mine ? my_row / share_h : 0, head = b.kv_head * share_h + my_row - token * share_h;
+            const RowResult<T> res(p, mine && whole, (int64_t)(b.from + token) * c.Hq + head, mr, lr);
 #pragma unroll
             for (int pass = 0; pass < Walk::VCH / PASS; ++pass) {
-                float o[PASS];
-                channels(pass, o);
-                if (mine)
+                if (pass + n > 0) __syncthreads();           // the pass before has been read
 #pragma unroll
-                    for (int e = 0; e < PASS; e += 4)
-                        *reinterpret_cast<f32x4*>(p.part_o + (slot * kCaRows + r) * DH + Walk::VCH * piece + pass * PASS + e) = f32x4{o[e], o[e + 1], o[e + 2], o[e + 3]};
+                for (int v = 0; v < 4; ++v)
+                    *reinterpret_cast<f32x4*>(&sums[wave][col][(4 * g + v) * PASS]) =
+                        f32x4{w.acc[n][pass * PASS][v] * f, w.acc[n][pass * PASS + 1][v] * f, w.acc[n][pass * PASS + 2][v] * f, w.acc[n][pass * PASS + 3][v] * f};
+                __syncthreads();
+                if (!mine) continue;
+                f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < WAVES; ++i) sum += *reinterpret_cast<const f32x4*>(&sums[i][r][piece * PASS]);
+                const int channel = Walk::VCH * piece + pass * PASS;
+                if (whole) {
+                    float o[PASS] = {sum.x, sum.y, sum.z, sum.w};
+                    res.store(p, DH, channel, o);
+                } else {
+                    *reinterpret_cast<f32x4*>(p.part_o + (slot * ROWS + 16 * n + r) * DH + channel) = sum;
+                }
             }
             if (mine && piece == 0) {
-                p.part_ml[(slot * kCaRows + r) * 2] = mr;
-                p.part_ml[(slot * kCaRows + r) * 2 + 1] = lr;
-            }
-            if (tile0 == 0) {
-                const int64_t last = (u + sp.tiles - 1) / share;         // the workgroup with the block's last tile
-                join = int4{(int)(last - blockIdx.x) + 1, b.row0, b.kv_head, s};
+                if (whole) {
+                    if (p.lse) p.lse[res.at] = res.lse;
+                } else {
+                    p.part_ml[(slot * ROWS + 16 * n + r) * 2] = mr;
+                    p.part_ml[(slot * ROWS + 16 * n + r) * 2 + 1] = lr;
+                }
             }
         }
+        if (!whole && tile0 == 0) join = CaJoin{(int)((u + tiles - 1) / share) - (int)blockIdx.x + 1, b.row0, b.n_rows, b.kv_head, b.from, {0, 0, 0}};      // up to the workgroup with the block's last tile
         u += count;
         __syncthreads();                         // before the next block's sums
     }
-    if (tid == 0) p.joins[blockIdx.x] = join;
+    if (CUT && tid == 0) p.joins[blockIdx.x] = join;
 }
 
-// The pieces of a row block that was cut, joined in the order of its tokens: a wavefront per row
-template <int DH, typename T>
+// The pieces of a row block that was cut, joined in the order of its tokens: row by row, a wavefront has every fourth piece, all of a wavefront's on their way at once
+template <int DH, typename T, int NT>
 __global__ __launch_bounds__(256) void cache_attn_join_kernel(const CacheAttnParams p) {
-    constexpr int N = DH / 64;
+    constexpr int N = DH / 64, ROWS = 16 * NT, U = 8;
+    __shared__ float ml[4][2];
+    __shared__ __align__(16) float sums[4][DH];
     const CacheStep& c = p.c;
-    const int4 join = p.joins[blockIdx.x];
-    const int pieces = join.x;
-    if (pieces == 0) return;
-    const int share_h = c.Hq / c.Hkv, lane = lane_id(), r = blockIdx.y * 4 + (threadIdx.x >> 6), s = join.w;
-    const int from = cache_row(c, s), n_rows = max(cache_row(c, s + 1) - from, 0) * share_h, row = join.y + r;
-    if (row >= n_rows) return;
-    const int token = row / share_h, head = join.z * share_h + row - token * share_h;
-    const int64_t first = blockIdx.x;
-    auto slot = [&](int i) { return (2 * (first + i) + (i == 0 ? 1 : 0)) * kCaRows + r; };
-    float m = -INFINITY, l = 0.f, o[N] = {};
-    for (int i0 = 0; i0 < pieces; i0 += 64) {
-        const int n = min(pieces - i0, 64);
-        const int64_t mine = slot(min(i0 + lane, pieces - 1));
-        const float mi = p.part_ml[2 * mine], li = p.part_ml[2 * mine + 1];
-        float top = mi;
-#pragma unroll
-        for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
-        top = fmaxf(top, m);
-        const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
-        const float f = mi == -INFINITY || lane >= n ? 0.f : __builtin_amdgcn_exp2f(mi - top);
-        l *= keep;
-#pragma unroll
-        for (int e = 0; e < N; ++e) o[e] *= keep;
-        m = top;
-        constexpr int U = 8;
-        for (int i = 0; i < n; i += U) {
-            float x[U][N];
+    const CaJoin join = p.joins[blockIdx.x];
+    if (join.pieces == 0) return;
+    const int share_h = c.Hq / c.Hkv, lane = lane_id(), wave = threadIdx.x >> 6;
+    const int rows = min(ROWS, join.n_rows - join.row0);
+    for (int r = blockIdx.y; r < rows; r += gridDim.y) {
+        auto slot = [&](int i) { return (2 * (int64_t)(blockIdx.x + i) + (i == 0 ? 1 : 0)) * ROWS + r; };
+        float m = -INFINITY, l = 0.f, o[N] = {};
+        for (int i0 = wave; i0 < join.pieces; i0 += 4 * U) {
+            float x[U][N], mi[U], li[U];
 #pragma unroll
             for (int k = 0; k < U; ++k) {
-                const float* at = p.part_o + slot(i0 + min(i + k, n - 1)) * DH + N * lane;
+                const int64_t at = slot(min(i0 + 4 * k, join.pieces - 1));
+                mi[k] = p.part_ml[2 * at];
+                li[k] = p.part_ml[2 * at + 1];
 #pragma unroll
-                for (int e = 0; e < N; ++e) x[k][e] = at[e];
+                for (int e = 0; e < N; ++e) x[k][e] = p.part_o[at * DH + N * lane + e];
             }
+            float top = m;
 #pragma unroll
             for (int k = 0; k < U; ++k) {
-                if (i + k >= n) break;
-                const float fk = __shfl(f, i + k);
-                l += __shfl(li, i + k) * fk;
-#pragma unroll
-                for (int e = 0; e < N; ++e) o[e] = fmaf(x[k][e], fk, o[e]);
+                if (i0 + 4 * k >= join.pieces) mi[k] = -INFINITY;
+                top = fmaxf(top, mi[k]);
             }
+            const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+            l *= keep;
+#pragma unroll
+            for (int e = 0; e < N; ++e) o[e] *= keep;
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                if (mi[k] == -INFINITY) continue;            // it saw nothing, or is not there
+                const float f = __builtin_amdgcn_exp2f(mi[k] - top);
+                l = fmaf(li[k], f, l);
+#pragma unroll
+                for (int e = 0; e < N; ++e) o[e] = fmaf(x[k][e], f, o[e]);
+            }
+            m = top;
+        }
+        __syncthreads();                         // the row before has been read
+        if (lane == 0) {
+            ml[wave][0] = m;
+            ml[wave][1] = l;
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) sums[wave][N * lane + e] = o[e];
+        __syncthreads();
+        if (threadIdx.x < DH / 4) {              // of one wavefront: the prior's lse is read by all before any writes in its place
+            const int ch = 4 * threadIdx.x;
+            float mr = ml[0][0], lr = 0.f, q[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 1; i < 4; ++i) mr = fmaxf(mr, ml[i][0]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (ml[i][0] == -INFINITY) continue;
+                const float f = __builtin_amdgcn_exp2f(ml[i][0] - mr);
+                lr = fmaf(ml[i][1], f, lr);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) q[e] = fmaf(sums[i][ch + e], f, q[e]);
+            }
+            const int row = join.row0 + r, token = row / share_h, head = join.kv_head * share_h + row - token * share_h;
+            const RowResult<T> res(p, true, (int64_t)(join.from + token) * c.Hq + head, mr, lr);
+            res.store(p, DH, ch, q);
+            if (p.lse && threadIdx.x == 0) p.lse[res.at] = res.lse;
         }
     }
-    const RowResult<T> res(p, (int64_t)(from + token) * c.Hq + head, m, l);
-    if constexpr (N == 1) {
-        float q = o[0] * res.wo;
-        const int64_t i = res.at * DH + lane;
-        if (res.wp != 0.f) q = fmaf(res.wp, as_float<T>(((const T*)p.prior_out)[i]), q);
-        if constexpr (sizeof(T) == 2) ((uint16_t*)p.out)[i] = f32_to_bf16_bits(q);
-        else ((float*)p.out)[i] = q;
-    } else {
-        res.store(p, DH, N * lane, o);
-    }
-    if (p.lse && lane == 0) p.lse[res.at] = res.lse;
 }
 
 // ---- host ---------------------------------------------------------------------------------------
-// The scratch array: sums [2 * workgroups][16 rows][dh], references and sums of weights [2 * workgroups][16][2], and what is to be joined [workgroups]
-struct CacheAttnScratch {
-    int wgs;
+// How a call is launched, by its descriptor, and the scratch array of a cut one: sums [2 * workgroups][rows][dh], references and sums of weights
+// [2 * workgroups][rows][2], and what is to be joined [workgroups]
+struct CacheAttnPlan {
+    int nt, wgs;
+    bool cut;
     size_t off_ml, off_joins, total;
 };
-static CacheAttnScratch cache_attn_scratch(const astra_cache_desc& d) {
-    CacheAttnScratch s{};
+template <int DH, typename T>
+static int cache_attn_wgs(int nt) {
+    return kCaCus * (nt == 1 ? CaShape<DH, T, 1, true>::wgs_per_cu : CaShape<DH, T, 2, true>::wgs_per_cu);
+}
+static int cache_attn_plan(const astra_cache_desc& d, CacheAttnPlan* pl) {
+    CacheAttnPlan s{};
     const bool f32 = d.dtype == ASTRA_F32;
-    s.wgs = kCaCus * (d.head_dim == 64    ? f32 ? kCaWgsPerCu<64, float> : kCaWgsPerCu<64, uint16_t>
-                      : d.head_dim == 128 ? f32 ? kCaWgsPerCu<128, float> : kCaWgsPerCu<128, uint16_t>
-                                          : f32 ? kCaWgsPerCu<256, float> : kCaWgsPerCu<256, uint16_t>);
-    // no more than the shares of the smallest size that there can be
-    const int64_t blocks = ((int64_t)d.n_tokens * (d.n_q_heads / d.n_kv_heads) / kCaRows + d.n_seqs) * d.n_kv_heads;
+    const int64_t rows = (int64_t)d.n_tokens * (d.n_q_heads / d.n_kv_heads);
+    // blocks of 32 rows where sequences have that many on average: half the walks over the cache
+    s.nt = !f32 && d.head_dim <= 128 && rows >= 32 * (int64_t)d.n_seqs ? 2 : 1;
     const int64_t tiles = ceil_div((int64_t)d.max_pages * d.page_size, kCaTile);
-    const int64_t most = blocks > (int64_t)s.wgs * kCaMinShare ? s.wgs : ceil_div(blocks * tiles, kCaMinShare);
-    if (most < s.wgs) s.wgs = (int)(most > 0 ? most : 1);
-    const size_t rows = (size_t)2 * s.wgs * kCaRows;
-    s.off_ml = align_up(rows * d.head_dim * 4, 256);
-    s.off_joins = s.off_ml + align_up(rows * 2 * 4, 256);
-    s.total = s.off_joins + align_up((size_t)s.wgs * sizeof(int4), 256);
-    return s;
+    const int64_t blocks = (rows / (16 * s.nt) + d.n_seqs) * d.n_kv_heads;               // no more than these
+    if (rows > (1 << 30) || blocks * tiles > 0x7fffffff) return ASTRA_ERR_UNSUPPORTED;   // rows and units are counted in 32 bits
+    s.cut = tiles > kCaMaxTiles;
+    s.wgs = (int)blocks;
+    if (s.cut) {
+        int most = d.head_dim == 64    ? f32 ? cache_attn_wgs<64, float>(s.nt) : cache_attn_wgs<64, uint16_t>(s.nt)
+                   : d.head_dim == 128 ? f32 ? cache_attn_wgs<128, float>(s.nt) : cache_attn_wgs<128, uint16_t>(s.nt)
+                                       : f32 ? cache_attn_wgs<256, float>(s.nt) : cache_attn_wgs<256, uint16_t>(s.nt);
+        const int64_t shares = ceil_div(blocks * tiles, kCaMinShare);
+        s.wgs = (int)(shares < most ? shares : most);
+        const size_t r = (size_t)2 * s.wgs * 16 * s.nt;
+        s.off_ml = align_up(r * d.head_dim * 4, 256);
+        s.off_joins = s.off_ml + align_up(r * 2 * 4, 256);
+        s.total = s.off_joins + align_up((size_t)s.wgs * sizeof(CaJoin), 256);
+    }
+    if (s.total == 0) s.total = 256;
+    *pl = s;
+    return ASTRA_OK;
 }
 
-template <int DH, typename T>
-static int launch_cache_attention(const CacheAttnParams& p, int wgs, hipStream_t s) {
-    cache_attn_kernel<DH, T><<<wgs, kCaThreads, 0, s>>>(p);
+template <int DH, typename T, int NT>
+static int launch_cache_attention(const CacheAttnParams& p, const CacheAttnPlan& pl, hipStream_t s) {
+    if (!pl.cut) {
+        cache_attn_kernel<DH, T, NT, false><<<pl.wgs, CaShape<DH, T, NT, false>::threads, 0, s>>>(p);
+        return launch_status();
+    }
+    cache_attn_kernel<DH, T, NT, true><<<pl.wgs, CaShape<DH, T, NT, true>::threads, 0, s>>>(p);
     const int rc = launch_status();
     if (rc) return rc;
-    cache_attn_join_kernel<DH, T><<<dim3(wgs, kCaRows / 4), 256, 0, s>>>(p);
+    cache_attn_join_kernel<DH, T, NT><<<dim3(pl.wgs, 4), 256, 0, s>>>(p);
     return launch_status();
 }
 
+template <int DH, typename T>
+static int launch_cache_attention(const CacheAttnParams& p, const CacheAttnPlan& pl, hipStream_t s) {
+    if constexpr (sizeof(T) == 2 && DH <= 128)
+        if (pl.nt == 2) return launch_cache_attention<DH, T, 2>(p, pl, s);
+    return launch_cache_attention<DH, T, 1>(p, pl, s);
+}
+
 template <typename T>
-static int launch_cache_attention(const CacheAttnParams& p, int dh, int wgs, hipStream_t s) {
-    if (dh == 64) return launch_cache_attention<64, T>(p, wgs, s);
-    if (dh == 128) return launch_cache_attention<128, T>(p, wgs, s);
-    return launch_cache_attention<256, T>(p, wgs, s);
+static int launch_cache_attention(const CacheAttnParams& p, int dh, const CacheAttnPlan& pl, hipStream_t s) {
+    if (dh == 64) return launch_cache_attention<64, T>(p, pl, s);
+    if (dh == 128) return launch_cache_attention<128, T>(p, pl, s);
+    return launch_cache_attention<256, T>(p, pl, s);
 }
 
 }  // namespace astra
@@ -671,20 +747,23 @@ using namespace astra;
 extern "C" {
 
 size_t astra_cache_attention_workspace_bytes(const astra_cache_desc* desc) {
-    if (check_cache_desc(desc) != ASTRA_OK) return 0;
-    return cache_attn_scratch(*desc).total;
+    CacheAttnPlan pl;
+    if (check_cache_desc(desc) != ASTRA_OK || cache_attn_plan(*desc, &pl) != ASTRA_OK) return 0;
+    return pl.total;
 }
 
 int astra_cache_attention(const astra_cache_desc* desc, const int32_t* page_table, const int32_t* lens, const int32_t* first_row,
                           const void* q, const uint8_t* k_pages, const uint8_t* v_pages, const float* k_scales, const float* v_scales,
                           const void* prior_out, const float* prior_lse, void* out, float* lse_out, void* workspace,
                           size_t workspace_bytes, void* stream) {
-    const int rc = check_cache_desc(desc);
+    int rc = check_cache_desc(desc);
+    if (rc) return rc;
+    CacheAttnPlan pl;
+    rc = cache_attn_plan(*desc, &pl);
     if (rc) return rc;
     if (desc->n_tokens == 0 || desc->n_seqs == 0) return ASTRA_OK;
     if (!page_table || !lens || !first_row || !q || !k_pages || !v_pages || !k_scales || !v_scales || !out || !prior_out != !prior_lse) return ASTRA_ERR_NULL;
-    const CacheAttnScratch sc = cache_attn_scratch(*desc);
-    if (!workspace || workspace_bytes < sc.total) return ASTRA_ERR_WORKSPACE;
+    if (!workspace || workspace_bytes < pl.total) return ASTRA_ERR_WORKSPACE;
     for (const void* a : {q, (const void*)k_pages, (const void*)v_pages, prior_out, (const void*)out, (const void*)workspace})
         if ((uintptr_t)a % 16 != 0) return ASTRA_ERR_UNSUPPORTED;
     CacheAttnParams p{};
@@ -694,10 +773,10 @@ int astra_cache_attention(const astra_cache_desc* desc, const int32_t* page_tabl
     p.q_stride = desc->q_stride ? desc->q_stride : desc->n_q_heads * desc->head_dim;
     p.scale = desc->scale != 0.f ? desc->scale : 1.f / sqrtf((float)desc->head_dim);
     p.part_o = (float*)workspace;
-    p.part_ml = (float*)((char*)workspace + sc.off_ml);
-    p.joins = (int4*)((char*)workspace + sc.off_joins);
-    if (desc->dtype == ASTRA_BF16) return launch_cache_attention<uint16_t>(p, desc->head_dim, sc.wgs, (hipStream_t)stream);
-    return launch_cache_attention<float>(p, desc->head_dim, sc.wgs, (hipStream_t)stream);
+    p.part_ml = (float*)((char*)workspace + pl.off_ml);
+    p.joins = (CaJoin*)((char*)workspace + pl.off_joins);
+    if (desc->dtype == ASTRA_BF16) return launch_cache_attention<uint16_t>(p, desc->head_dim, pl, (hipStream_t)stream);
+    return launch_cache_attention<float>(p, desc->head_dim, pl, (hipStream_t)stream);
 }
 
 }  // extern "C"

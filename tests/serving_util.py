@@ -9,13 +9,13 @@ from paper_2505_19342_amd import workloads as wl
 class Step:
     """Sequences with `lens` cached and `new` new tokens; pages that hold nothing yet are full of NaN codes and their scales NaN."""
 
-    def __init__(self, dtype, hq, hkv, dh, page, lens, new, seed=0, behind=0, spread=(-8, -5), std=1.3):
+    def __init__(self, dtype, hq, hkv, dh, page, lens, new, seed=0, behind=0, spread=(-8, -5), std=1.3, columns=0):
         rng = self.rng = np.random.default_rng(seed)
         self.dtype, self.hq, self.hkv, self.dh, self.page = dtype, hq, hkv, dh, page
         self.rnd = wl.round_to_bf16 if dtype == "bf16" else (lambda a: np.asarray(a, np.float32))
         held = [-(-(a + b) // page) for a, b in zip(lens, new)]
         self.n_pages = sum(held) + 2
-        self.table = np.full((len(lens), max(held + [1]) + 1), -1, np.int32)
+        self.table = np.full((len(lens), max(held + [1, columns - 1]) + 1), -1, np.int32)
         ids = iter(rng.permutation(self.n_pages))
         for s, h in enumerate(held):
             self.table[s, :h] = [next(ids) for _ in range(h)]

@@ -125,12 +125,17 @@ def test_append_in_many_steps_is_the_prompt():
 @pytest.mark.parametrize("dtype, heads", [("bf16", (8, 2, 128)), ("bf16", (3, 3, 64)), ("bf16", (20, 1, 64)), ("bf16", (4, 4, 256)), ("f32", (6, 2, 64)), ("f32", (8, 1, 128)),
                                           ("f32", (2, 1, 256))])
 def test_attention_of_single_tokens(dtype, heads, page):
-    check_attention(Step(dtype, *heads, page, [0, 1, 15, 16, 17, 31, 32, 200, 0, 333], [1, 1, 1, 1, 1, 1, 1, 1, 0, 1], seed=page, behind=2).fill())
+    """Where sequences cannot be long, and where they could (the table is wide: row blocks are dealt out in shares)."""
+    for columns in (0, 4096 // page):
+        check_attention(Step(dtype, *heads, page, [0, 1, 15, 16, 17, 31, 32, 200, 0, 333], [1, 1, 1, 1, 1, 1, 1, 1, 0, 1], seed=page, behind=2, columns=columns).fill())
 
 
 @pytest.mark.parametrize("dtype, heads, page", [("bf16", (8, 2, 128), 64), ("bf16", (3, 3, 64), 16), ("bf16", (5, 1, 128), 32), ("f32", (6, 2, 64), 32), ("bf16", (4, 2, 256), 128)])
 def test_attention_of_several_tokens(dtype, heads, page):
-    check_attention(Step(dtype, *heads, page, [0, 50, 7, 100], [37, 3, 0, 70], seed=page, behind=1).fill())
+    """Blocks of 16 and of 32 rows (many rows per sequence, bf16, heads of up to 128)."""
+    for columns in (0, 4096 // page):
+        check_attention(Step(dtype, *heads, page, [0, 50, 7, 100], [37, 3, 0, 70], seed=page, behind=1, columns=columns).fill())
+        check_attention(Step(dtype, *heads, page, [0, 150], [3, 2], seed=page, columns=columns).fill())
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -139,9 +144,12 @@ def test_attention_of_long_and_uneven_contexts(dtype):
     check_attention(Step(dtype, 4, 4, 64, 16, [3001], [2], seed=9).fill(), scale=0.3)
 
 
-def test_attention_joined_to_a_prior_result():
-    for dtype in ("bf16", "f32"):
-        st = Step(dtype, 8, 2, 128, 32, [70, 0, 900, 3], [1, 2, 1, 1], seed=10, behind=1).fill()
+@pytest.mark.parametrize("columns", [0, 128])
+@pytest.mark.parametrize("dh", [64, 128, 256])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_joined_to_a_prior_result(dtype, dh, columns):
+    for new in ([1, 2, 1, 1], [1, 2, 1, 30]):
+        st = Step(dtype, 8, 2, dh, 32, [70, 0, 900, 3], new, seed=10, behind=1, columns=columns).fill()
         prior = st.rnd(st.rng.standard_normal(st.q.shape).astype(np.float32))
         lse = (st.rng.standard_normal((st.n, st.hq)) + 6).astype(np.float32)
         lse[0, :3], prior[0, 0] = -np.inf, np.nan                       # a prior over nothing counts for nothing, whatever it holds
@@ -151,8 +159,22 @@ def test_attention_joined_to_a_prior_result():
         check_attention(st, prior, lse)
 
 
-def test_attention_leaves_pages_out():
-    st = Step("bf16", 4, 2, 128, 16, [100, 40, 60], [1, 3, 20], seed=11).fill()
+@pytest.mark.parametrize("n", [64, 65, 200, 1024])
+@pytest.mark.parametrize("columns", [0, 130])
+def test_attention_of_many_sequences(n, columns):
+    rng = np.random.default_rng(n)
+    lens, new = rng.integers(0, 60, n), rng.integers(0, 3, n)
+    check_attention(Step("bf16", 2, 1, 64, 16, lens.tolist(), new.tolist(), seed=n, behind=1, columns=columns).fill())
+
+
+def test_a_row_block_in_many_pieces_and_many_blocks_in_a_share():
+    check_attention(Step("f32", 2, 1, 64, 128, [20000, 3], [1, 1], seed=3).fill())
+    check_attention(Step("bf16", 16, 16, 64, 128, [100] * 40, [1] * 40, seed=4, columns=64).fill())
+
+
+@pytest.mark.parametrize("columns", [0, 200])
+def test_attention_leaves_pages_out(columns):
+    st = Step("bf16", 4, 2, 128, 16, [100, 40, 60], [1, 3, 20], seed=11, columns=columns).fill()
     st.table[0, 2], st.table[0, 6], st.table[1], st.table[2, 0] = -5, st.n_pages, -1, 2 ** 31 - 1
     check_attention(st)
 
@@ -173,8 +195,8 @@ def test_attention_with_lengths_that_nothing_backs():
 
 
 def test_nan_values_reach_only_the_rows_that_see_them():
-    for dtype in ("bf16", "f32"):
-        st = Step(dtype, 4, 2, 128, 16, [40], [9], seed=13).fill()
+    for dtype, columns in (("bf16", 0), ("f32", 0), ("bf16", 200), ("f32", 200)):
+        st = Step(dtype, 4, 2, 128, 16, [40], [9], seed=13, columns=columns).fill()
         p = st.table[0, 45 // 16]
         st.pages[1][p, 1, 45 % 16, 70] = 0xff                           # a new token's value is NaN in one channel
         st.pages[0][st.table[0, 47 // 16], 0, 47 % 16, 3] = 0x7f        # and a later one's key

@@ -1,19 +1,20 @@
 // Products of a few tokens with weights of 4 bits and a scale per group of columns (include/astra.h, astra_w4_linear).
 #include "common.h"
 
+#include <algorithm>
+
 namespace astra {
 
 // ------------------------------------------------------------------------------------------------
 // y[t, n] = bias[n] + sum_g scale[n, g] ( sum_{k in g} (16 + code) x  -  (16 + zero) sum_{k in g} x )
 // The weights are what has to be read, so the products run on the matrix cores with 16 rows of the weights on the N side and 16 tokens on the M side, and the
 // codes reach them in two operations for two: the four bits go to the upper mantissa bits of a bf16 16.0, which makes it 16 + code
-// exactly.  A lane loads 16 bytes of a row, 32 columns; the four lanes of a row then trade words (permlane swaps: a 4 x 4 transpose), so that
-// one 16x16x32 MFMA sees 32 neighbouring columns of every row, all of one group.  A group's sum stays in fp32 and takes the row's scale there;
+// exactly.  One 16x16x32 MFMA sees 32 neighbouring columns of every row, all of one group.  A group's sum stays in fp32 and takes the row's scale there;
 // the sum of x over the group comes from another MFMA, against ones.  fp32 tokens are sums of three bf16 parts (8 + 8 + 8 mantissa bits), and their weights
 // code - 8, at 20 operations for eight instead of 8: the difference of the two sums above loses three bits, which a bf16 result does not show.
-// The wavefronts of a workgroup take blocks of 128 columns in turn, U of them at a time with all their loads on the way, and add up in LDS.
-// TT x RT: tiles of 16 tokens and of 16 rows that a workgroup has; more rows for many tokens, whose x otherwise passes the second-level caches more often
-// than the weights pass memory.
+// What a lane loads and what it multiplies are not the same: sixteen neighbouring lanes of an operand belong to sixteen rows, and a load that reaches sixteen
+// places takes four times the first-level cache's cycles of one that reaches four.  Lanes load neighbouring pieces of a row (four lanes a row of
+// the weights, 16 or 32 lanes a token) and the operands are read from LDS, where x lies already cut into parts and in the order of the weights.
 // ------------------------------------------------------------------------------------------------
 struct W4Params {
     const void* x;
@@ -28,23 +29,21 @@ struct W4Params {
 
 __device__ __forceinline__ f32x4 mfma_16x16x32(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
-// word i of lane group j <-> word j of lane group i (groups of 16 lanes)
-__device__ __forceinline__ u32x4 transpose_words(u32x4 w) {
-    auto a = __builtin_amdgcn_permlane32_swap(w.x, w.z, false, false);      // upper half of the first <-> lower half of the second
-    auto b = __builtin_amdgcn_permlane32_swap(w.y, w.w, false, false);
-    auto c = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);    // odd rows of the first <-> even rows of the second
-    auto d = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
-    return u32x4{(uint32_t)c[0], (uint32_t)c[1], (uint32_t)d[0], (uint32_t)d[1]};
-}
 constexpr float kOffset = 16.f;
-// eight codes as 16 + code, in the order 0 4 1 5 2 6 3 7
-__device__ __forceinline__ bf16x8 weights_offset(uint32_t w) {
-    constexpr uint32_t kMask = 0x00780078u, kSixteen = 0x41804180u;
+// Eight codes as 16 + code, in the order 0 4 1 5 2 6 3 7.  The constants are kept where one instruction can have both (as literals they are two).
+struct OffsetConstants {
+    uint32_t mask = 0x00780078u, sixteen = 0x41804180u;
+    __device__ __forceinline__ OffsetConstants() {
+        asm volatile("" : "+s"(mask));
+        asm volatile("" : "+v"(sixteen));
+    }
+};
+__device__ __forceinline__ bf16x8 weights_offset(uint32_t w, const OffsetConstants& c) {
     u32x4 o;
-    o.x = ((w << 3) & kMask) | kSixteen;
-    o.y = ((w >> 1) & kMask) | kSixteen;
-    o.z = ((w >> 5) & kMask) | kSixteen;
-    o.w = ((w >> 9) & kMask) | kSixteen;
+    o.x = ((w << 3) & c.mask) | c.sixteen;
+    o.y = ((w >> 1) & c.mask) | c.sixteen;
+    o.z = ((w >> 5) & c.mask) | c.sixteen;
+    o.w = ((w >> 9) & c.mask) | c.sixteen;
     return __builtin_bit_cast(bf16x8, o);
 }
 // eight codes as (code - 8) / 16, in order
@@ -63,138 +62,67 @@ template <typename T>
 struct Tokens;
 template <>
 struct Tokens<uint16_t> {
+    static constexpr int kParts = 1;
     u32x4 w;
     __device__ __forceinline__ void load(const uint16_t* p) { w = *reinterpret_cast<const u32x4*>(p); }
-    __device__ __forceinline__ void operand(bf16x8 (&a)[1]) const {
-        u32x4 o;
-        o.x = __builtin_amdgcn_perm(w.z, w.x, 0x05040100u);
-        o.y = __builtin_amdgcn_perm(w.z, w.x, 0x07060302u);
-        o.z = __builtin_amdgcn_perm(w.w, w.y, 0x05040100u);
-        o.w = __builtin_amdgcn_perm(w.w, w.y, 0x07060302u);
-        a[0] = __builtin_bit_cast(bf16x8, o);
+    __device__ __forceinline__ void parts(bool there, u32x4 (&a)[1]) const {
+        const u32x4 x = there ? w : u32x4{0u, 0u, 0u, 0u};
+        a[0].x = __builtin_amdgcn_perm(x.z, x.x, 0x05040100u);
+        a[0].y = __builtin_amdgcn_perm(x.z, x.x, 0x07060302u);
+        a[0].z = __builtin_amdgcn_perm(x.w, x.y, 0x05040100u);
+        a[0].w = __builtin_amdgcn_perm(x.w, x.y, 0x07060302u);
     }
 };
 template <>
 struct Tokens<float> {
+    static constexpr int kParts = 3;
     f32x4 w[2];
     __device__ __forceinline__ void load(const float* p) {
         w[0] = reinterpret_cast<const f32x4*>(p)[0];
         w[1] = reinterpret_cast<const f32x4*>(p)[1];
     }
-    __device__ __forceinline__ void operand(bf16x8 (&a)[3]) const {
+    __device__ __forceinline__ void parts(bool there, u32x4 (&a)[3]) const {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            float v = w[e >> 2][e & 3];
+        for (int e = 0; e < 8; e += 2) {
+            float v0 = there ? w[e >> 2][e & 3] : 0.f, v1 = there ? w[e >> 2][(e & 3) + 1] : 0.f;
 #pragma unroll
             for (int i = 0; i < 3; ++i) {                  // every difference is exact
-                const float part = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
-                a[i][e] = (__bf16)part;
-                v -= part;
+                a[i][e >> 1] = __builtin_amdgcn_perm(__float_as_uint(v1), __float_as_uint(v0), 0x07060302u);
+                v0 -= __uint_as_float(__float_as_uint(v0) & 0xffff0000u);
+                v1 -= __uint_as_float(__float_as_uint(v1) & 0xffff0000u);
             }
         }
     }
 };
+// the four lanes of a row each have one value: all four to all of them
+__device__ __forceinline__ void spread(uint32_t v, uint32_t (&out)[4]) {
+    const auto h = __builtin_amdgcn_permlane32_swap(v, v, false, false);        // lanes 0 .. 31 twice, lanes 32 .. 63 twice
+    const auto a = __builtin_amdgcn_permlane16_swap(h[0], h[0], false, false), b = __builtin_amdgcn_permlane16_swap(h[1], h[1], false, false);
+    out[0] = a[0];
+    out[1] = a[1];
+    out[2] = b[0];
+    out[3] = b[1];
+}
 
+// an element as it lies in memory, converted where it is used: a conversion beside the load is a wait there
+template <typename T>
+__device__ __forceinline__ uint32_t raw_element(const void* p, int64_t i) {
+    if constexpr (sizeof(T) == 2) return ((const uint16_t*)p)[i];
+    else return ((const uint32_t*)p)[i];
+}
+template <typename T>
+__device__ __forceinline__ float from_raw(uint32_t w) { return __uint_as_float(sizeof(T) == 2 ? w << 16 : w); }
 template <typename T>
 __device__ __forceinline__ float element(const void* p, int64_t i) {
     if constexpr (sizeof(T) == 2) return bf16_bits_to_f32(((const uint16_t*)p)[i]);
     else return ((const float*)p)[i];
 }
 
-// GS: log2 of the group.  blockIdx.x: tile of 16 * RT rows, blockIdx.y: tile of 16 * TT tokens
-template <typename T, int TT, int RT, int GS, int U>
-__global__ __launch_bounds__(TT * RT > 2 ? 512 : 1024) void w4_kernel(const W4Params p) {
-    constexpr bool F32 = sizeof(T) == 4;
-    constexpr int PARTS = F32 ? 3 : 1, NG = 128 >> GS, STEPS = 4 / NG;      // groups in a block, products of 32 columns in a group
-    extern __shared__ __align__(16) float sums[];                           // [wavefronts][RT][16][16]
+// Sums of the wavefronts in order, and the store: tiles of 16 tokens one after the other.  The caller's rows are n0 .. n0 + 16 * RT - 1, its tokens t0 .. t0 + 16 * TT - 1;
+// sums: [wavefronts][16][16 * RT] floats
+template <typename T, int TT, int RT>
+__device__ __forceinline__ void store_sums(const W4Params& p, float* sums, int wave, int waves, int64_t t0, int n0, const f32x4 (&acc)[TT][RT]) {
     const int lane = lane_id(), col = lane & 15, g = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-    const int n0 = blockIdx.x * 16 * RT;
-    const int64_t t0 = (int64_t)blockIdx.y * 16 * TT;
-    const int groups = p.K >> GS, blocks = (p.K + 127) >> 7;
-    const uint8_t* rows[RT];
-    int64_t scale_at[RT];
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        const int64_t n = min(n0 + 16 * r + col, p.N - 1);
-        rows[r] = p.codes + n * (p.K >> 1) + 16 * g;
-        scale_at[r] = n * groups;
-    }
-    const T* x[TT];
-    bool there[TT];
-#pragma unroll
-    for (int i = 0; i < TT; ++i) {
-        there[i] = t0 + 16 * i + col < p.n_tokens;
-        x[i] = (const T*)p.x + min(t0 + 16 * i + col, p.n_tokens - 1) * p.x_stride + 8 * g;
-    }
-    const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
-    f32x4 acc[TT][RT] = {};
-
-    for (int b0 = wave; b0 < blocks; b0 += waves * U) {
-        u32x4 w[U][RT];
-        float scale[U][RT][NG], zero[U][RT][NG];
-        Tokens<T> xs[U][4][TT];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            // a block beyond the last, and words and groups beyond the last column: read where there is something, counted for nothing (x is 0, and so is the scale)
-            const int k0 = min(b0 + u * waves, blocks - 1) * 128;
-#pragma unroll
-            for (int r = 0; r < RT; ++r) w[u][r] = *reinterpret_cast<const u32x4*>(rows[r] + (min(k0, p.K - 32 - 32 * g) >> 1));
-#pragma unroll
-            for (int a = 0; a < 4; ++a)
-#pragma unroll
-                for (int i = 0; i < TT; ++i) {
-                    xs[u][a][i] = Tokens<T>{};
-                    if (there[i] && b0 + u * waves < blocks && k0 + 32 * a < p.K) xs[u][a][i].load(x[i] + k0 + 32 * a);
-                }
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int j = 0; j < NG; ++j) {
-                    const int at = (k0 >> GS) + j, in = min(at, groups - 1);
-                    scale[u][r][j] = at == in ? element<T>(p.scales, scale_at[r] + in) : 0.f;
-                    zero[u][r][j] = p.zeros ? (float)(p.zeros[scale_at[r] + in] & 15) : 8.f;
-                }
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-#pragma unroll
-            for (int r = 0; r < RT; ++r) w[u][r] = transpose_words(w[u][r]);
-#pragma unroll
-            for (int j = 0; j < NG; ++j) {
-                f32x4 d[TT][RT] = {}, sum[TT] = {};
-#pragma unroll
-                for (int st = 0; st < STEPS; ++st) {
-                    const int a = j * STEPS + st;
-                    bf16x8 wf[RT];
-#pragma unroll
-                    for (int r = 0; r < RT; ++r) wf[r] = F32 ? weights_exact(w[u][r][a]) : weights_offset(w[u][r][a]);
-#pragma unroll
-                    for (int i = 0; i < TT; ++i) {
-                        bf16x8 xa[PARTS];
-                        xs[u][a][i].operand(xa);
-#pragma unroll
-                        for (int k = 0; k < PARTS; ++k) {
-#pragma unroll
-                            for (int r = 0; r < RT; ++r) d[i][r] = mfma_16x16x32(xa[k], wf[r], d[i][r]);
-                            if (!F32 || p.zeros) sum[i] = mfma_16x16x32(xa[k], ones, sum[i]);
-                        }
-                    }
-                }
-#pragma unroll
-                for (int r = 0; r < RT; ++r) {
-                    const float s = F32 ? 16.f * scale[u][r][j] : scale[u][r][j];
-                    const float z = F32 ? (zero[u][r][j] - 8.f) * 0.0625f : zero[u][r][j] + kOffset;
-#pragma unroll
-                    for (int i = 0; i < TT; ++i)
-#pragma unroll
-                        for (int v = 0; v < 4; ++v) acc[i][r][v] = fmaf(s, fmaf(-z, sum[i][v], d[i][r][v]), acc[i][r][v]);
-                }
-            }
-        }
-    }
-
-    // the wavefronts' sums in order: RT tiles of 16 tokens at a time
 #pragma unroll
     for (int i = 0; i < TT; ++i) {
         if (i > 0) __syncthreads();
@@ -215,6 +143,135 @@ __global__ __launch_bounds__(TT * RT > 2 ? 512 : 1024) void w4_kernel(const W4Pa
     }
 }
 
+constexpr int kW4RowBytes = 80;                    // of a row's 64 bytes in LDS: sixteen rows' words of one column fall into different banks
+template <typename T, int TP, int U>
+struct W4Lds {                                     // of a wavefront
+    static constexpr int x_stride = U * 256 + 16;  // bytes of a token's part: sixteen tokens' pieces of one column fall into different banks
+    static constexpr int x_bytes = Tokens<T>::kParts * TP * x_stride, w_bytes = U * 16 * kW4RowBytes, all = x_bytes + w_bytes;
+};
+
+// Few tokens: a workgroup has 16 rows of the weights and TP <= 16 tokens, its wavefronts take U neighbouring blocks of 128 columns in turn; a batch's loads are on
+// their way while the one before is worked on.  GS: log2 of the group; blockIdx.y: tile of 16 tokens
+template <typename T, int TP, int GS, int U>
+__global__ __launch_bounds__(1024) void w4_kernel(const W4Params p) {
+    constexpr bool F32 = sizeof(T) == 4;
+    constexpr int PARTS = Tokens<T>::kParts, NG = 128 >> GS, STEPS = 4 / NG;      // groups in a block, products of 32 columns in a group
+    constexpr int GROUPS = U * NG, NS = (GROUPS + 3) / 4;                         // groups in a batch, loads for their scales
+    constexpr int PIECES = U * 16, NX = (TP * PIECES + 63) / 64;                  // pieces of eight columns of a token in a batch, and of a lane
+    using Lds = W4Lds<T, TP, U>;
+    extern __shared__ __align__(16) char w4_lds[];
+    const int lane = lane_id(), col = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const int n0 = blockIdx.x * 16;
+    const int64_t t0 = (int64_t)blockIdx.y * 16;
+    const int tokens = (int)min(p.n_tokens - t0, (int64_t)TP);
+    const int groups = p.K >> GS, batches = (p.K + 128 * U - 1) / (128 * U);
+    char* const lds_x = w4_lds + wave * Lds::all;
+    char* const lds_w = lds_x + Lds::x_bytes;
+
+    // what this lane loads: a piece of a row (row lane / 4), the scale of group g of a row (row lane % 16), pieces of tokens: offsets from what the workgroup has first
+    const uint8_t* const codes = p.codes + (int64_t)n0 * (p.K >> 1);
+    const char* const scales = (const char*)p.scales + (int64_t)n0 * groups * (int)sizeof(T);
+    const uint8_t* const zeros = p.zeros + (int64_t)n0 * groups;
+    const char* const x = (const char*)p.x + t0 * p.x_stride * (int)sizeof(T);
+    const int last_row = p.N - 1 - n0;
+    const uint32_t w_at = (uint32_t)min(lane >> 2, last_row) * (uint32_t)(p.K >> 1) + 16u * (lane & 3);
+    const uint32_t group_at = (uint32_t)min(col, last_row) * (uint32_t)groups;
+    uint32_t x_at[NX];
+#pragma unroll
+    for (int i = 0; i < NX; ++i) {
+        const int id = i * 64 + lane;
+        x_at[i] = ((uint32_t)min(id / PIECES, tokens - 1) * (uint32_t)p.x_stride + 8u * (id % PIECES)) * (uint32_t)sizeof(T);
+    }
+
+    u32x4 raw_w[U];
+    uint32_t raw_scale[NS], raw_zero[NS];
+    Tokens<T> raw_x[NX];
+    auto load = [&](int batch) __attribute__((always_inline)) {
+        const int k0 = batch * 128 * U;
+        const uint8_t* const wk = codes + (k0 >> 1);
+        const char* const xk = x + (int64_t)k0 * (int)sizeof(T);
+        // columns beyond the last: read where there is something, counted for nothing (x is 0 there, and so is the scale)
+        const bool all = k0 + 128 * U <= p.K;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            uint32_t at = w_at + 64u * u;
+            if (!all) at = (uint32_t)((int)w_at + min(64 * u, ((p.K - 32 - k0) >> 1) - 16 * (lane & 3)));
+            raw_w[u] = *reinterpret_cast<const u32x4*>(wk + (all ? (int64_t)at : (int64_t)(int)at));
+        }
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+            const uint32_t at = group_at + (uint32_t)min((k0 >> GS) + 4 * i + g, groups - 1);
+            raw_scale[i] = raw_element<T>(scales, at);
+            if (p.zeros) raw_zero[i] = zeros[at];
+        }
+#pragma unroll
+        for (int i = 0; i < NX; ++i) {
+            int back = 0;
+            if (!all) back = max(8 * ((i * 64 + lane) % PIECES) - (p.K - 8 - k0), 0) * (int)sizeof(T);
+            raw_x[i].load(reinterpret_cast<const T*>(xk + (int64_t)x_at[i] - back));
+        }
+    };
+    const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
+    const OffsetConstants constants;
+    f32x4 acc[1][1] = {};
+    int batch = wave;
+    if (batch < batches) load(batch);
+    while (batch < batches) {
+        // to LDS, a wavefront's own part: its reads come after its writes, nobody else is waited for
+#pragma unroll
+        for (int u = 0; u < U; ++u) *reinterpret_cast<u32x4*>(lds_w + (u * 16 + (lane >> 2)) * kW4RowBytes + 16 * (lane & 3)) = raw_w[u];
+#pragma unroll
+        for (int i = 0; i < NX; ++i) {
+            const int id = i * 64 + lane, token = id / PIECES, piece = id % PIECES;
+            u32x4 a[PARTS];
+            raw_x[i].parts(batch * 128 * U + 128 * U <= p.K || batch * 128 * U + 8 * piece < p.K, a);
+            if (TP * PIECES % 64 == 0 || token < TP)
+#pragma unroll
+                for (int k = 0; k < PARTS; ++k) *reinterpret_cast<u32x4*>(lds_x + (k * TP + token) * Lds::x_stride + 16 * piece) = a[k];
+        }
+        float scale[NS][4], zero[NS][4];
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+            uint32_t s[4], z[4];
+            spread((batch * 128 * U >> GS) + 4 * i + g < groups ? raw_scale[i] : 0u, s);
+            if (p.zeros) spread(raw_zero[i], z);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float sc = from_raw<T>(s[j]), zr = p.zeros ? (float)(z[j] & 15u) : 8.f;
+                scale[i][j] = F32 ? 16.f * sc : sc;
+                zero[i][j] = F32 ? (zr - 8.f) * 0.0625f : zr + kOffset;
+            }
+        }
+        const int next = batch + waves;
+        if (next < batches) load(next);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < NG; ++j) {
+                f32x4 d = {0.f, 0.f, 0.f, 0.f}, sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int a = j * STEPS; a < (j + 1) * STEPS; ++a) {
+                    const uint32_t w = *reinterpret_cast<const uint32_t*>(lds_w + (u * 16 + col) * kW4RowBytes + 16 * a + 4 * g);
+                    const bf16x8 wf = F32 ? weights_exact(w) : weights_offset(w, constants);
+#pragma unroll
+                    for (int k = 0; k < PARTS; ++k) {
+                        // lanes of tokens that are not there have some other's, or what is left of an earlier call: their rows of the result are dropped
+                        const bf16x8 xa = *reinterpret_cast<const bf16x8*>(lds_x + (k * TP + min(col, TP - 1)) * Lds::x_stride + u * 256 + 64 * a + 16 * g);
+                        d = mfma_16x16x32(xa, wf, d);
+                        if (!F32 || p.zeros) sum = mfma_16x16x32(xa, ones, sum);
+                    }
+                }
+                const int i = (u * NG + j) >> 2, jj = (u * NG + j) & 3;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) acc[0][0][v] = fmaf(scale[i][jj], fmaf(-zero[i][jj], sum[v], d[v]), acc[0][0][v]);
+            }
+        batch = next;
+    }
+    __syncthreads();                               // everybody is through with its part of LDS
+    store_sums<T, 1, 1>(p, (float*)w4_lds, wave, waves, t0, n0, acc);
+}
+
 // ---- host ---------------------------------------------------------------------------------------
 static int check_w4_desc(const astra_w4_desc* d) {
     if (!d) return ASTRA_ERR_NULL;
@@ -224,30 +281,41 @@ static int check_w4_desc(const astra_w4_desc* d) {
     if (d->in_features > (1 << 24) || d->out_features > (1 << 24)) return ASTRA_ERR_UNSUPPORTED;
     if (d->x_stride != 0) {
         if (d->x_stride < d->in_features) return ASTRA_ERR_SHAPE;
+        if (d->x_stride > (1 << 25)) return ASTRA_ERR_UNSUPPORTED;
         if ((int64_t)d->x_stride * elem_bytes(d->dtype) % 16 != 0) return ASTRA_ERR_UNSUPPORTED;
     }
     return ASTRA_OK;
 }
 
-template <typename T, int TT, int RT, int U>
-static int launch_w4(const W4Params& p, int waves, hipStream_t s) {
-    const int64_t nx = ceil_div(p.N, 16 * RT), ny = ceil_div(p.n_tokens, 16 * TT);
+template <typename T, int TP, int GS, int U>
+static int launch_w4(const W4Params& p, hipStream_t s) {
+    static std::atomic<uint64_t> allowed{0};
+    using Lds = W4Lds<T, TP, U>;
+    const int batches = (int)ceil_div(p.K, 128 * U), most = TP > 8 ? 8 : 16, waves = batches < most ? batches : most;
+    const int64_t nx = ceil_div(p.N, 16), ny = ceil_div(p.n_tokens, 16);
     if (nx > 0x7fffffff || ny > 65535) return ASTRA_ERR_SHAPE;
-    const dim3 grid((unsigned)nx, (unsigned)ny);
-    const size_t lds = (size_t)waves * RT * 256 * sizeof(float);
-    if (p.group_shift == 5) w4_kernel<T, TT, RT, 5, U><<<grid, waves * kWave, lds, s>>>(p);
-    else if (p.group_shift == 6) w4_kernel<T, TT, RT, 6, U><<<grid, waves * kWave, lds, s>>>(p);
-    else w4_kernel<T, TT, RT, 7, U><<<grid, waves * kWave, lds, s>>>(p);
+    const int lds = std::max(waves * Lds::all, waves * 256 * (int)sizeof(float));
+    if (lds > 64 * 1024) {
+        const int rc = allow_dynamic_lds(allowed, reinterpret_cast<const void*>(&w4_kernel<T, TP, GS, U>), most * Lds::all);
+        if (rc) return rc;
+    }
+    w4_kernel<T, TP, GS, U><<<dim3((unsigned)nx, (unsigned)ny), waves * kWave, lds, s>>>(p);
     return launch_status();
+}
+
+template <typename T, int TP>
+static int launch_w4(const W4Params& p, hipStream_t s) {
+    constexpr int U = sizeof(T) == 2 ? 2 : 1;
+    if (p.group_shift == 5) return launch_w4<T, TP, 5, U>(p, s);
+    if (p.group_shift == 6) return launch_w4<T, TP, 6, U>(p, s);
+    return launch_w4<T, TP, 7, U>(p, s);
 }
 
 template <typename T>
 static int launch_w4(const W4Params& p, hipStream_t s) {
-    const int blocks = (int)ceil_div(p.K, 128);
-    const int waves = blocks <= 4 ? 4 : blocks <= 32 ? 8 : 16;
-    if (p.n_tokens <= 16) return launch_w4<T, 1, 1, 2>(p, waves, s);
-    if (sizeof(T) == 4 || p.n_tokens <= 32) return launch_w4<T, 2, 1, 1>(p, waves, s);
-    return launch_w4<uint16_t, 4, 2, 1>(p, 8, s);
+    if (p.n_tokens <= 2) return launch_w4<T, 2>(p, s);
+    if (p.n_tokens <= 8) return launch_w4<T, 8>(p, s);
+    return launch_w4<T, 16>(p, s);
 }
 
 }  // namespace astra

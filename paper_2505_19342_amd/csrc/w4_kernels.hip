@@ -272,6 +272,146 @@ __global__ __launch_bounds__(1024) void w4_kernel(const W4Params p) {
     store_sums<T, 1, 1>(p, (float*)w4_lds, wave, waves, t0, n0, acc);
 }
 
+// More tokens (bf16): a workgroup has 16 * RT * WR rows and 16 * TT tokens.  Its wavefronts are WK groups, which take chunks of 128 columns in turn, of WR, which have
+// 16 * RT rows each and read x from one copy of it in LDS, with the sums of x over the groups beside it.  While a chunk is worked on the next one's x and codes are on their
+// way.  What bounds it: the operations that make operands of codes, and x, which passes the second-level caches once for every 16 * RT * WR rows.
+template <int TT, int WR, int WK, int RT, int GS>
+struct W4Wide {
+    static constexpr int waves = WR * WK, threads = waves * kWave;
+    static constexpr int x_bytes = TT * 4 * 1024;                               // [tile][32 columns][lane of the operand] 16 bytes
+    static constexpr int sum_bytes = (128 >> GS) * TT * 16 * 4;                 // [group][token]
+    static constexpr int w_bytes = RT * 16 * kW4RowBytes;
+    static constexpr int of_group = x_bytes + sum_bytes, all = WK * of_group + waves * w_bytes;
+    static constexpr int lds = all > waves * RT * 1024 ? all : waves * RT * 1024;
+};
+
+template <int TT, int WR, int WK, int RT, int GS>
+__global__ __launch_bounds__((W4Wide<TT, WR, WK, RT, GS>::threads), 2) void w4_wide_kernel(const W4Params p) {
+    using Shape = W4Wide<TT, WR, WK, RT, GS>;
+    constexpr int NG = 128 >> GS, STEPS = 4 / NG, NS = (NG + 3) / 4;
+    constexpr int LANES = WR * kWave;                                            // of a group of wavefronts
+    constexpr int NX = TT * 16 * 16 / LANES;                                     // pieces of eight columns of a token that a lane brings to LDS
+    extern __shared__ __align__(16) char w4_lds[];
+    const int lane = lane_id(), col = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wk = wave / WR, wr = wave % WR;
+    const int n0 = (blockIdx.x * WR + wr) * 16 * RT, groups = p.K >> GS;
+    const int64_t t0 = (int64_t)blockIdx.y * 16 * TT;
+    const int chunks = (p.K + 127) >> 7, rounds = (chunks + WK - 1) / WK;        // every wavefront goes round as often
+    char* const lds_x = w4_lds + wk * Shape::of_group;
+    float* const lds_sum = (float*)(lds_x + Shape::x_bytes);
+    char* const lds_w = w4_lds + WK * Shape::of_group + wave * Shape::w_bytes;
+    const int id = wr * kWave + lane, piece = id & 15, tok = id >> 4;            // lanes of a token are neighbours; the next pieces are LANES / 16 tokens on
+
+    u32x4 raw_w[RT];
+    uint32_t raw_scale[RT][NS], raw_zero[RT][NS];
+    Tokens<uint16_t> raw_x[NX];
+    auto load = [&](int chunk) __attribute__((always_inline)) {
+        // a chunk beyond the last, and columns beyond the last: read where there is something, counted for nothing (x is 0 there, and so is the scale)
+        const int k0 = min(chunk, chunks - 1) * 128;
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            const int64_t row = min(n0 + 16 * r + (lane >> 2), p.N - 1);
+            raw_w[r] = *reinterpret_cast<const u32x4*>(p.codes + row * (p.K >> 1) + (min(k0 + 32 * (lane & 3), p.K - 32) >> 1));
+        }
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int i = 0; i < NS; ++i) {
+                const int64_t at = (int64_t)min(n0 + 16 * r + col, p.N - 1) * groups + min((k0 >> GS) + min(4 * i + g, NG - 1), groups - 1);
+                raw_scale[r][i] = raw_element<uint16_t>(p.scales, at);
+                if (p.zeros) raw_zero[r][i] = p.zeros[at];
+            }
+#pragma unroll
+        for (int i = 0; i < NX; ++i) {
+            const int64_t t = min(t0 + tok + i * (LANES / 16), p.n_tokens - 1);
+            raw_x[i].load((const uint16_t*)p.x + t * p.x_stride + min(k0 + 8 * piece, p.K - 8));
+        }
+    };
+    const OffsetConstants constants;
+    f32x4 acc[TT][RT] = {};
+    load(wk);
+    for (int round = 0; round < rounds; ++round) {
+        const int chunk = round * WK + wk, k0 = chunk * 128;
+        if (round > 0) __syncthreads();                       // the chunk before has been read
+#pragma unroll
+        for (int i = 0; i < NX; ++i) {
+            u32x4 a[1];
+            raw_x[i].parts(k0 + 8 * piece < p.K, a);
+            const int t = tok + i * (LANES / 16), slot = ((piece & 3) * 16 + ((t & 15) ^ piece)) * 16;       // exchanged within sixteen: a token's pieces in different banks
+            *reinterpret_cast<u32x4*>(lds_x + ((t >> 4) * 4 + (piece >> 2)) * 1024 + slot) = a[0];
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum += __uint_as_float(a[0][e] << 16) + __uint_as_float(a[0][e] & 0xffff0000u);
+#pragma unroll
+            for (int o = 1; o < (1 << GS) / 8; o <<= 1) sum += __shfl_xor(sum, o);
+            if ((piece & ((1 << GS) / 8 - 1)) == 0) lds_sum[(piece >> (GS - 3)) * TT * 16 + t] = sum;
+        }
+#pragma unroll
+        for (int r = 0; r < RT; ++r) *reinterpret_cast<u32x4*>(lds_w + (r * 16 + (lane >> 2)) * kW4RowBytes + 16 * (lane & 3)) = raw_w[r];
+        float scale[RT][NG], zero[RT][NG];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            uint32_t s[4], z[4];
+            spread(raw_scale[r][0], s);
+            if (p.zeros) spread(raw_zero[r][0], z);
+#pragma unroll
+            for (int j = 0; j < NG; ++j) {
+                scale[r][j] = (k0 >> GS) + j < groups ? from_raw<uint16_t>(s[j]) : 0.f;
+                zero[r][j] = (p.zeros ? (float)(z[j] & 15u) : 8.f) + kOffset;
+            }
+        }
+        if (round + 1 < rounds) load(chunk + WK);
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < NG; ++j) {
+            f32x4 d[TT][RT] = {};
+#pragma unroll
+            for (int a = j * STEPS; a < (j + 1) * STEPS; ++a) {
+                bf16x8 wf[RT];
+#pragma unroll
+                for (int r = 0; r < RT; ++r) wf[r] = weights_offset(*reinterpret_cast<const uint32_t*>(lds_w + (r * 16 + col) * kW4RowBytes + 16 * a + 4 * g), constants);
+#pragma unroll
+                for (int i = 0; i < TT; ++i) {
+                    const bf16x8 xa = *reinterpret_cast<const bf16x8*>(lds_x + (i * 4 + a) * 1024 + (g * 16 + (col ^ (4 * a + g))) * 16);
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) d[i][r] = mfma_16x16x32(xa, wf[r], d[i][r]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < TT; ++i) {
+                const f32x4 sum = *reinterpret_cast<const f32x4*>(lds_sum + (j * TT + i) * 16 + 4 * g);
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) acc[i][r][v] = fmaf(scale[r][j], fmaf(-zero[r][j], sum[v], d[i][r][v]), acc[i][r][v]);
+            }
+        }
+    }
+    __syncthreads();
+    // the groups' sums in order, a tile of tokens at a time
+    float* const sums = (float*)w4_lds;
+    constexpr int ROWS = 16 * RT * WR;
+#pragma unroll
+    for (int i = 0; i < TT; ++i) {
+        if (i > 0) __syncthreads();
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) sums[(wk * 16 + 4 * g + v) * ROWS + (wr * RT + r) * 16 + col] = acc[i][r][v];
+        __syncthreads();
+        for (int e = threadIdx.x; e < 16 * ROWS; e += Shape::threads) {
+            const int64_t t = t0 + 16 * i + e / ROWS;
+            const int n = blockIdx.x * ROWS + e % ROWS;
+            if (t >= p.n_tokens || n >= p.N) continue;
+            float y = p.bias ? element<uint16_t>(p.bias, n) : 0.f;
+#pragma unroll
+            for (int k = 0; k < WK; ++k) y += sums[k * 16 * ROWS + e];
+            if (p.y_bf16) ((uint16_t*)p.y)[t * p.N + n] = f32_to_bf16_bits(y);
+            else ((float*)p.y)[t * p.N + n] = y;
+        }
+    }
+}
+
 // ---- host ---------------------------------------------------------------------------------------
 static int check_w4_desc(const astra_w4_desc* d) {
     if (!d) return ASTRA_ERR_NULL;
@@ -311,10 +451,42 @@ static int launch_w4(const W4Params& p, hipStream_t s) {
     return launch_w4<T, TP, 7, U>(p, s);
 }
 
+template <int TT, int WR, int WK, int RT, int GS>
+static int launch_w4_wide(const W4Params& p, hipStream_t s) {
+    static std::atomic<uint64_t> allowed{0};
+    using Shape = W4Wide<TT, WR, WK, RT, GS>;
+    const int64_t nx = ceil_div(p.N, 16 * RT * WR), ny = ceil_div(p.n_tokens, 16 * TT);
+    if (nx > 0x7fffffff || ny > 65535) return ASTRA_ERR_SHAPE;
+    if (Shape::lds > 64 * 1024) {
+        const int rc = allow_dynamic_lds(allowed, reinterpret_cast<const void*>(&w4_wide_kernel<TT, WR, WK, RT, GS>), Shape::lds);
+        if (rc) return rc;
+    }
+    w4_wide_kernel<TT, WR, WK, RT, GS><<<dim3((unsigned)nx, (unsigned)ny), Shape::threads, Shape::lds, s>>>(p);
+    return launch_status();
+}
+
+template <int TT, int WR, int WK, int RT>
+static int launch_w4_wide(const W4Params& p, hipStream_t s) {
+    if (p.group_shift == 5) return launch_w4_wide<TT, WR, WK, RT, 5>(p, s);
+    if (p.group_shift == 6) return launch_w4_wide<TT, WR, WK, RT, 6>(p, s);
+    return launch_w4_wide<TT, WR, WK, RT, 7>(p, s);
+}
+
+template <int TT>
+static int launch_w4_wide(const W4Params& p, hipStream_t s) {
+    // tiles of 128 rows where those are enough for the units, of 32 otherwise
+    if (ceil_div(p.N, 128) * ceil_div(p.n_tokens, 16 * TT) >= 192) return launch_w4_wide<TT, 4, 2, 2>(p, s);
+    return launch_w4_wide<TT, 2, 4, 1>(p, s);
+}
+
 template <typename T>
 static int launch_w4(const W4Params& p, hipStream_t s) {
     if (p.n_tokens <= 2) return launch_w4<T, 2>(p, s);
     if (p.n_tokens <= 8) return launch_w4<T, 8>(p, s);
+    if constexpr (sizeof(T) == 2) {
+        if (p.n_tokens > 32) return launch_w4_wide<4>(p, s);
+        if (p.n_tokens > 16) return launch_w4_wide<2>(p, s);
+    }
     return launch_w4<T, 16>(p, s);
 }
 

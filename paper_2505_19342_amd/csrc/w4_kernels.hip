@@ -2,6 +2,7 @@
 #include "common.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace astra {
 
@@ -94,16 +95,6 @@ struct Tokens<float> {
         }
     }
 };
-// the four lanes of a row each have one value: all four to all of them
-__device__ __forceinline__ void spread(uint32_t v, uint32_t (&out)[4]) {
-    const auto h = __builtin_amdgcn_permlane32_swap(v, v, false, false);        // lanes 0 .. 31 twice, lanes 32 .. 63 twice
-    const auto a = __builtin_amdgcn_permlane16_swap(h[0], h[0], false, false), b = __builtin_amdgcn_permlane16_swap(h[1], h[1], false, false);
-    out[0] = a[0];
-    out[1] = a[1];
-    out[2] = b[0];
-    out[3] = b[1];
-}
-
 // an element as it lies in memory, converted where it is used: a conversion beside the load is a wait there
 template <typename T>
 __device__ __forceinline__ uint32_t raw_element(const void* p, int64_t i) {
@@ -143,20 +134,57 @@ __device__ __forceinline__ void store_sums(const W4Params& p, float* sums, int w
     }
 }
 
+// Scales and zero points of 16 rows for 16 neighbouring groups, on their way through a wavefront's part of LDS: sixteen lanes load the sixteen of a row (a lane per row and
+// group would reach sixty-four places at a time), and each lane reads those of its row where a group ends.
+template <typename T>
+struct ScaleSpan {
+    static constexpr int kGroups = 16;
+    using Raw = std::conditional_t<sizeof(T) == 2, uint16_t, uint32_t>;
+    static constexpr int kStride = sizeof(T) == 2 ? 18 : 17, kZeroStride = 20;      // rows start in different banks
+    static constexpr int kScaleBytes = 16 * kStride * (int)sizeof(Raw), kBytes = (kScaleBytes + 16 * kZeroStride + 15) / 16 * 16;
+    Raw s[4];
+    uint8_t z[4];
+    // rows n0 .. n0 + 15 (those beyond the last: the last), groups from `first` on (beyond the last: the last)
+    __device__ __forceinline__ void load(const W4Params& p, int n0, int groups, int first) {
+        const int lane = lane_id(), at = min(first + (lane & 15), groups - 1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t j = (int64_t)min(n0 + 4 * i + (lane >> 4), p.N - 1) * groups + at;
+            s[i] = ((const Raw*)p.scales)[j];
+            if (p.zeros) z[i] = p.zeros[j];
+        }
+    }
+    __device__ __forceinline__ void put(const W4Params& p, char* lds) const {
+        const int lane = lane_id();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            ((Raw*)lds)[(4 * i + (lane >> 4)) * kStride + (lane & 15)] = s[i];
+            if (p.zeros) ((uint8_t*)lds + kScaleBytes)[(4 * i + (lane >> 4)) * kZeroStride + (lane & 15)] = z[i];
+        }
+    }
+    // of row lane % 16
+    __device__ __forceinline__ static float scale(const char* lds, int group) { return from_raw<T>(((const Raw*)lds)[(lane_id() & 15) * kStride + group]); }
+    __device__ __forceinline__ static float zero(const W4Params& p, const char* lds, int group) {
+        return p.zeros ? (float)(((const uint8_t*)lds + kScaleBytes)[(lane_id() & 15) * kZeroStride + group] & 15) : 8.f;
+    }
+};
+
 constexpr int kW4RowBytes = 80;                    // of a row's 64 bytes in LDS: sixteen rows' words of one column fall into different banks
 template <typename T, int TP, int U>
 struct W4Lds {                                     // of a wavefront
     static constexpr int x_stride = U * 256 + 16;  // bytes of a token's part: sixteen tokens' pieces of one column fall into different banks
-    static constexpr int x_bytes = Tokens<T>::kParts * TP * x_stride, w_bytes = U * 16 * kW4RowBytes, all = x_bytes + w_bytes;
+    static constexpr int x_bytes = Tokens<T>::kParts * TP * x_stride, w_bytes = U * 16 * kW4RowBytes, all = x_bytes + w_bytes + ScaleSpan<T>::kBytes;
 };
 
-// Few tokens: a workgroup has 16 rows of the weights and TP <= 16 tokens, its wavefronts take U neighbouring blocks of 128 columns in turn; a batch's loads are on
-// their way while the one before is worked on.  GS: log2 of the group; blockIdx.y: tile of 16 tokens
+// Few tokens: a workgroup has 16 rows of the weights and TP <= 16 tokens, each of its wavefronts a range of columns; it takes U neighbouring blocks of 128 at a time, and a
+// batch's loads are on their way while the one before is worked on.  GS: log2 of the group; blockIdx.y: tile of 16 tokens
+template <int TP, int GS>
+constexpr int kW4MaxWaves = TP > 8 || GS == 5 ? 8 : 16;      // what registers leave room for
 template <typename T, int TP, int GS, int U>
-__global__ __launch_bounds__(1024) void w4_kernel(const W4Params p) {
+__global__ __launch_bounds__((kW4MaxWaves<TP, GS> * kWave)) void w4_kernel(const W4Params p) {
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int PARTS = Tokens<T>::kParts, NG = 128 >> GS, STEPS = 4 / NG;      // groups in a block, products of 32 columns in a group
-    constexpr int GROUPS = U * NG, NS = (GROUPS + 3) / 4;                         // groups in a batch, loads for their scales
+    constexpr int GROUPS = U * NG, PER_SPAN = ScaleSpan<T>::kGroups / GROUPS;       // groups in a batch, batches whose scales are brought together
     constexpr int PIECES = U * 16, NX = (TP * PIECES + 63) / 64;                  // pieces of eight columns of a token in a batch, and of a lane
     using Lds = W4Lds<T, TP, U>;
     extern __shared__ __align__(16) char w4_lds[];
@@ -168,15 +196,13 @@ __global__ __launch_bounds__(1024) void w4_kernel(const W4Params p) {
     const int groups = p.K >> GS, batches = (p.K + 128 * U - 1) / (128 * U);
     char* const lds_x = w4_lds + wave * Lds::all;
     char* const lds_w = lds_x + Lds::x_bytes;
+    char* const lds_s = lds_w + Lds::w_bytes;
 
-    // what this lane loads: a piece of a row (row lane / 4), the scale of group g of a row (row lane % 16), pieces of tokens: offsets from what the workgroup has first
+    // what this lane loads: a piece of a row (row lane / 4), pieces of tokens: offsets from what the workgroup has first
     const uint8_t* const codes = p.codes + (int64_t)n0 * (p.K >> 1);
-    const char* const scales = (const char*)p.scales + (int64_t)n0 * groups * (int)sizeof(T);
-    const uint8_t* const zeros = p.zeros + (int64_t)n0 * groups;
     const char* const x = (const char*)p.x + t0 * p.x_stride * (int)sizeof(T);
     const int last_row = p.N - 1 - n0;
     const uint32_t w_at = (uint32_t)min(lane >> 2, last_row) * (uint32_t)(p.K >> 1) + 16u * (lane & 3);
-    const uint32_t group_at = (uint32_t)min(col, last_row) * (uint32_t)groups;
     uint32_t x_at[NX];
 #pragma unroll
     for (int i = 0; i < NX; ++i) {
@@ -185,7 +211,7 @@ __global__ __launch_bounds__(1024) void w4_kernel(const W4Params p) {
     }
 
     u32x4 raw_w[U];
-    uint32_t raw_scale[NS], raw_zero[NS];
+    ScaleSpan<T> span;
     Tokens<T> raw_x[NX];
     auto load = [&](int batch) __attribute__((always_inline)) {
         const int k0 = batch * 128 * U;
@@ -200,12 +226,6 @@ __global__ __launch_bounds__(1024) void w4_kernel(const W4Params p) {
             raw_w[u] = *reinterpret_cast<const u32x4*>(wk + (all ? (int64_t)at : (int64_t)(int)at));
         }
 #pragma unroll
-        for (int i = 0; i < NS; ++i) {
-            const uint32_t at = group_at + (uint32_t)min((k0 >> GS) + 4 * i + g, groups - 1);
-            raw_scale[i] = raw_element<T>(scales, at);
-            if (p.zeros) raw_zero[i] = zeros[at];
-        }
-#pragma unroll
         for (int i = 0; i < NX; ++i) {
             int back = 0;
             if (!all) back = max(8 * ((i * 64 + lane) % PIECES) - (p.K - 8 - k0), 0) * (int)sizeof(T);
@@ -215,9 +235,17 @@ __global__ __launch_bounds__(1024) void w4_kernel(const W4Params p) {
     const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
     const OffsetConstants constants;
     f32x4 acc[1][1] = {};
-    int batch = wave;
-    if (batch < batches) load(batch);
-    while (batch < batches) {
+    const int per_wave = (batches + waves - 1) / waves, begin = min(wave * per_wave, batches), end = min(begin + per_wave, batches);
+    if (begin < end) {
+        span.load(p, n0, groups, begin * GROUPS);
+        load(begin);
+    }
+    for (int batch = begin; batch < end; ++batch) {
+        const int in_span = (batch - begin) % PER_SPAN;
+        if (in_span == 0) {
+            span.put(p, lds_s);
+            if (batch + PER_SPAN < end) span.load(p, n0, groups, (batch + PER_SPAN) * GROUPS);
+        }
         // to LDS, a wavefront's own part: its reads come after its writes, nobody else is waited for
 #pragma unroll
         for (int u = 0; u < U; ++u) *reinterpret_cast<u32x4*>(lds_w + (u * 16 + (lane >> 2)) * kW4RowBytes + 16 * (lane & 3)) = raw_w[u];
@@ -230,21 +258,7 @@ __global__ __launch_bounds__(1024) void w4_kernel(const W4Params p) {
 #pragma unroll
                 for (int k = 0; k < PARTS; ++k) *reinterpret_cast<u32x4*>(lds_x + (k * TP + token) * Lds::x_stride + 16 * piece) = a[k];
         }
-        float scale[NS][4], zero[NS][4];
-#pragma unroll
-        for (int i = 0; i < NS; ++i) {
-            uint32_t s[4], z[4];
-            spread((batch * 128 * U >> GS) + 4 * i + g < groups ? raw_scale[i] : 0u, s);
-            if (p.zeros) spread(raw_zero[i], z);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float sc = from_raw<T>(s[j]), zr = p.zeros ? (float)(z[j] & 15u) : 8.f;
-                scale[i][j] = F32 ? 16.f * sc : sc;
-                zero[i][j] = F32 ? (zr - 8.f) * 0.0625f : zr + kOffset;
-            }
-        }
-        const int next = batch + waves;
-        if (next < batches) load(next);
+        if (batch + 1 < end) load(batch + 1);
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -262,33 +276,57 @@ __global__ __launch_bounds__(1024) void w4_kernel(const W4Params p) {
                         if (!F32 || p.zeros) sum = mfma_16x16x32(xa, ones, sum);
                     }
                 }
-                const int i = (u * NG + j) >> 2, jj = (u * NG + j) & 3;
+                const int in = in_span * GROUPS + u * NG + j;
+                const float zr = ScaleSpan<T>::zero(p, lds_s, in);
+                float sc = ScaleSpan<T>::scale(lds_s, in);
+                if (batch * GROUPS + u * NG + j >= groups) sc = 0.f;
+                const float s = F32 ? 16.f * sc : sc, z = F32 ? (zr - 8.f) * 0.0625f : zr + kOffset;
 #pragma unroll
-                for (int v = 0; v < 4; ++v) acc[0][0][v] = fmaf(scale[i][jj], fmaf(-zero[i][jj], sum[v], d[v]), acc[0][0][v]);
+                for (int v = 0; v < 4; ++v) acc[0][0][v] = fmaf(s, fmaf(-z, sum[v], d[v]), acc[0][0][v]);
             }
-        batch = next;
     }
     __syncthreads();                               // everybody is through with its part of LDS
     store_sums<T, 1, 1>(p, (float*)w4_lds, wave, waves, t0, n0, acc);
 }
 
-// More tokens (bf16): a workgroup has 16 * RT * WR rows and 16 * TT tokens.  Its wavefronts are WK groups, which take chunks of 128 columns in turn, of WR, which have
-// 16 * RT rows each and read x from one copy of it in LDS, with the sums of x over the groups beside it.  While a chunk is worked on the next one's x and codes are on their
-// way.  What bounds it: the operations that make operands of codes, and x, which passes the second-level caches once for every 16 * RT * WR rows.
+// More tokens (bf16): a workgroup has 16 * RT * WR rows and 16 * TT tokens.  Its wavefronts are WK groups, each with a range of columns, of WR, which have
+// 16 * RT rows each and read x from one copy of it in LDS, with the sums of x over the groups beside it.  While a chunk of 128 columns is worked on, the next one goes to the other
+// half of LDS and the one after it is on its way from memory.  What bounds it: the operations that make operands of codes and scale the sums, and x, which passes the second-level
+// caches once for every 16 * RT * WR rows.
 template <int TT, int WR, int WK, int RT, int GS>
 struct W4Wide {
     static constexpr int waves = WR * WK, threads = waves * kWave;
     static constexpr int x_bytes = TT * 4 * 1024;                               // [tile][32 columns][lane of the operand] 16 bytes
     static constexpr int sum_bytes = (128 >> GS) * TT * 16 * 4;                 // [group][token]
-    static constexpr int w_bytes = RT * 16 * kW4RowBytes;
-    static constexpr int of_group = x_bytes + sum_bytes, all = WK * of_group + waves * w_bytes;
+    static constexpr int of_group = x_bytes + sum_bytes;
+    static constexpr int w_bytes = RT * 16 * kW4RowBytes, span_bytes = RT * ScaleSpan<uint16_t>::kBytes;
+    static constexpr int all = 2 * WK * of_group + waves * (2 * w_bytes + span_bytes);
     static constexpr int lds = all > waves * RT * 1024 ? all : waves * RT * 1024;
+    static_assert(lds <= 160 * 1024, "LDS of a unit");
 };
+
+// sum of eight bf16 values
+__device__ __forceinline__ float sum_eight(u32x4 w) {
+    const bf16x2 one = {(__bf16)1.f, (__bf16)1.f};
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t two = w[e];                 // a bit cast of a vector's element itself takes the first one
+        s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), one, s, false);
+    }
+    return s;
+}
+// v and that of another lane of the sixteen, by the number's bits: 0xB1, 0x4E exchange lanes 1 and 2 apart, 0x141 and 0x140 mirror eight and sixteen
+template <int CTRL>
+__device__ __forceinline__ float add_dpp(float v) {
+    return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
 
 template <int TT, int WR, int WK, int RT, int GS>
 __global__ __launch_bounds__((W4Wide<TT, WR, WK, RT, GS>::threads), 2) void w4_wide_kernel(const W4Params p) {
     using Shape = W4Wide<TT, WR, WK, RT, GS>;
-    constexpr int NG = 128 >> GS, STEPS = 4 / NG, NS = (NG + 3) / 4;
+    using Span = ScaleSpan<uint16_t>;
+    constexpr int NG = 128 >> GS, STEPS = 4 / NG, PER_SPAN = Span::kGroups / NG;
     constexpr int LANES = WR * kWave;                                            // of a group of wavefronts
     constexpr int NX = TT * 16 * 16 / LANES;                                     // pieces of eight columns of a token that a lane brings to LDS
     extern __shared__ __align__(16) char w4_lds[];
@@ -296,98 +334,105 @@ __global__ __launch_bounds__((W4Wide<TT, WR, WK, RT, GS>::threads), 2) void w4_w
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wk = wave / WR, wr = wave % WR;
     const int n0 = (blockIdx.x * WR + wr) * 16 * RT, groups = p.K >> GS;
     const int64_t t0 = (int64_t)blockIdx.y * 16 * TT;
-    const int chunks = (p.K + 127) >> 7, rounds = (chunks + WK - 1) / WK;        // every wavefront goes round as often
-    char* const lds_x = w4_lds + wk * Shape::of_group;
-    float* const lds_sum = (float*)(lds_x + Shape::x_bytes);
-    char* const lds_w = w4_lds + WK * Shape::of_group + wave * Shape::w_bytes;
+    const int chunks = (p.K + 127) >> 7, rounds = (chunks + WK - 1) / WK, first = wk * rounds;       // every wavefront goes round as often
+    char* const lds_x = w4_lds + wk * 2 * Shape::of_group;
+    char* const lds_w = w4_lds + WK * 2 * Shape::of_group + wave * (2 * Shape::w_bytes + Shape::span_bytes);
+    char* const lds_s = lds_w + 2 * Shape::w_bytes;
     const int id = wr * kWave + lane, piece = id & 15, tok = id >> 4;            // lanes of a token are neighbours; the next pieces are LANES / 16 tokens on
 
+    const uint8_t* codes[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) codes[r] = p.codes + (int64_t)min(n0 + 16 * r + (lane >> 2), p.N - 1) * (p.K >> 1) + 16 * (lane & 3);
+    const uint16_t* xs[NX];
+#pragma unroll
+    for (int i = 0; i < NX; ++i) xs[i] = (const uint16_t*)p.x + min(t0 + tok + i * (LANES / 16), p.n_tokens - 1) * p.x_stride + 8 * piece;
+
     u32x4 raw_w[RT];
-    uint32_t raw_scale[RT][NS], raw_zero[RT][NS];
+    Span span[RT];
     Tokens<uint16_t> raw_x[NX];
     auto load = [&](int chunk) __attribute__((always_inline)) {
         // a chunk beyond the last, and columns beyond the last: read where there is something, counted for nothing (x is 0 there, and so is the scale)
         const int k0 = min(chunk, chunks - 1) * 128;
+        const int wk0 = min(k0, p.K - 32 - 32 * (lane & 3)) >> 1, xk0 = min(k0, p.K - 8 - 8 * piece);
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            const int64_t row = min(n0 + 16 * r + (lane >> 2), p.N - 1);
-            raw_w[r] = *reinterpret_cast<const u32x4*>(p.codes + row * (p.K >> 1) + (min(k0 + 32 * (lane & 3), p.K - 32) >> 1));
-        }
+        for (int r = 0; r < RT; ++r) raw_w[r] = *reinterpret_cast<const u32x4*>(codes[r] + wk0);
 #pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int i = 0; i < NS; ++i) {
-                const int64_t at = (int64_t)min(n0 + 16 * r + col, p.N - 1) * groups + min((k0 >> GS) + min(4 * i + g, NG - 1), groups - 1);
-                raw_scale[r][i] = raw_element<uint16_t>(p.scales, at);
-                if (p.zeros) raw_zero[r][i] = p.zeros[at];
-            }
-#pragma unroll
-        for (int i = 0; i < NX; ++i) {
-            const int64_t t = min(t0 + tok + i * (LANES / 16), p.n_tokens - 1);
-            raw_x[i].load((const uint16_t*)p.x + t * p.x_stride + min(k0 + 8 * piece, p.K - 8));
-        }
+        for (int i = 0; i < NX; ++i) raw_x[i].load(xs[i] + xk0);
     };
-    const OffsetConstants constants;
-    f32x4 acc[TT][RT] = {};
-    load(wk);
-    for (int round = 0; round < rounds; ++round) {
-        const int chunk = round * WK + wk, k0 = chunk * 128;
-        if (round > 0) __syncthreads();                       // the chunk before has been read
+    auto stage = [&](int chunk, int half) __attribute__((always_inline)) {
+        char* const to = lds_x + half * Shape::of_group;
+        const bool there = chunk * 128 + 8 * piece < p.K;
 #pragma unroll
         for (int i = 0; i < NX; ++i) {
             u32x4 a[1];
-            raw_x[i].parts(k0 + 8 * piece < p.K, a);
+            raw_x[i].parts(there, a);
             const int t = tok + i * (LANES / 16), slot = ((piece & 3) * 16 + ((t & 15) ^ piece)) * 16;       // exchanged within sixteen: a token's pieces in different banks
-            *reinterpret_cast<u32x4*>(lds_x + ((t >> 4) * 4 + (piece >> 2)) * 1024 + slot) = a[0];
-            float sum = 0.f;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sum += __uint_as_float(a[0][e] << 16) + __uint_as_float(a[0][e] & 0xffff0000u);
-#pragma unroll
-            for (int o = 1; o < (1 << GS) / 8; o <<= 1) sum += __shfl_xor(sum, o);
-            if ((piece & ((1 << GS) / 8 - 1)) == 0) lds_sum[(piece >> (GS - 3)) * TT * 16 + t] = sum;
+            *reinterpret_cast<u32x4*>(to + ((t >> 4) * 4 + (piece >> 2)) * 1024 + slot) = a[0];
+            float sum = add_dpp<0x4E>(add_dpp<0xB1>(sum_eight(a[0])));
+            if constexpr (GS > 5) sum = add_dpp<0x141>(sum);
+            if constexpr (GS > 6) sum = add_dpp<0x140>(sum);
+            if ((piece & ((1 << GS) / 8 - 1)) == 0) ((float*)(to + Shape::x_bytes))[(piece >> (GS - 3)) * TT * 16 + t] = sum;
         }
 #pragma unroll
-        for (int r = 0; r < RT; ++r) *reinterpret_cast<u32x4*>(lds_w + (r * 16 + (lane >> 2)) * kW4RowBytes + 16 * (lane & 3)) = raw_w[r];
-        float scale[RT][NG], zero[RT][NG];
+        for (int r = 0; r < RT; ++r) *reinterpret_cast<u32x4*>(lds_w + half * Shape::w_bytes + (r * 16 + (lane >> 2)) * kW4RowBytes + 16 * (lane & 3)) = raw_w[r];
+    };
+    const OffsetConstants constants;
+    f32x4 acc[TT][RT] = {};
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            uint32_t s[4], z[4];
-            spread(raw_scale[r][0], s);
-            if (p.zeros) spread(raw_zero[r][0], z);
+    for (int r = 0; r < RT; ++r) span[r].load(p, n0 + 16 * r, groups, first * NG);
+    load(first);
+    stage(first, 0);
+    load(first + 1);
+    __syncthreads();
+    for (int round = 0; round < rounds; ++round) {
+        const int chunk = first + round, half = round & 1, in_span = round % PER_SPAN;
+        if (in_span == 0) {
 #pragma unroll
-            for (int j = 0; j < NG; ++j) {
-                scale[r][j] = (k0 >> GS) + j < groups ? from_raw<uint16_t>(s[j]) : 0.f;
-                zero[r][j] = (p.zeros ? (float)(z[j] & 15u) : 8.f) + kOffset;
+            for (int r = 0; r < RT; ++r) {
+                span[r].put(p, lds_s + r * Span::kBytes);
+                if (round + PER_SPAN < rounds) span[r].load(p, n0 + 16 * r, groups, (chunk + PER_SPAN) * NG);
             }
         }
-        if (round + 1 < rounds) load(chunk + WK);
-        __syncthreads();
+        if (round + 1 < rounds) {
+            stage(chunk + 1, half ^ 1);
+            load(chunk + 2);
+        }
+        const char* const x = lds_x + half * Shape::of_group;
+        const char* const w = lds_w + half * Shape::w_bytes;
 #pragma unroll
         for (int j = 0; j < NG; ++j) {
+            __builtin_amdgcn_sched_barrier(0);             // one group's operands at a time: registers
             f32x4 d[TT][RT] = {};
 #pragma unroll
             for (int a = j * STEPS; a < (j + 1) * STEPS; ++a) {
                 bf16x8 wf[RT];
 #pragma unroll
-                for (int r = 0; r < RT; ++r) wf[r] = weights_offset(*reinterpret_cast<const uint32_t*>(lds_w + (r * 16 + col) * kW4RowBytes + 16 * a + 4 * g), constants);
+                for (int r = 0; r < RT; ++r) wf[r] = weights_offset(*reinterpret_cast<const uint32_t*>(w + (r * 16 + col) * kW4RowBytes + 16 * a + 4 * g), constants);
 #pragma unroll
                 for (int i = 0; i < TT; ++i) {
-                    const bf16x8 xa = *reinterpret_cast<const bf16x8*>(lds_x + (i * 4 + a) * 1024 + (g * 16 + (col ^ (4 * a + g))) * 16);
+                    const bf16x8 xa = *reinterpret_cast<const bf16x8*>(x + (i * 4 + a) * 1024 + (g * 16 + (col ^ (4 * a + g))) * 16);
 #pragma unroll
                     for (int r = 0; r < RT; ++r) d[i][r] = mfma_16x16x32(xa, wf[r], d[i][r]);
                 }
             }
+            float s[RT], z[RT];
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                s[r] = Span::scale(lds_s + r * Span::kBytes, in_span * NG + j);
+                if (chunk * NG + j >= groups) s[r] = 0.f;
+                z[r] = Span::zero(p, lds_s + r * Span::kBytes, in_span * NG + j) + kOffset;
+            }
 #pragma unroll
             for (int i = 0; i < TT; ++i) {
-                const f32x4 sum = *reinterpret_cast<const f32x4*>(lds_sum + (j * TT + i) * 16 + 4 * g);
+                const f32x4 sum = *reinterpret_cast<const f32x4*>(x + Shape::x_bytes + ((j * TT + i) * 16 + 4 * g) * 4);
 #pragma unroll
                 for (int r = 0; r < RT; ++r)
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) acc[i][r][v] = fmaf(scale[r][j], fmaf(-zero[r][j], sum[v], d[i][r][v]), acc[i][r][v]);
+                    for (int v = 0; v < 4; ++v) acc[i][r][v] = fmaf(s[r], fmaf(-z[r], sum[v], d[i][r][v]), acc[i][r][v]);
             }
         }
+        __syncthreads();                       // this half has been read, the other is whole
     }
-    __syncthreads();
     // the groups' sums in order, a tile of tokens at a time
     float* const sums = (float*)w4_lds;
     constexpr int ROWS = 16 * RT * WR;
@@ -431,7 +476,7 @@ template <typename T, int TP, int GS, int U>
 static int launch_w4(const W4Params& p, hipStream_t s) {
     static std::atomic<uint64_t> allowed{0};
     using Lds = W4Lds<T, TP, U>;
-    const int batches = (int)ceil_div(p.K, 128 * U), most = TP > 8 ? 8 : 16, waves = batches < most ? batches : most;
+    const int batches = (int)ceil_div(p.K, 128 * U), most = kW4MaxWaves<TP, GS>, waves = batches < most ? batches : most;
     const int64_t nx = ceil_div(p.N, 16), ny = ceil_div(p.n_tokens, 16);
     if (nx > 0x7fffffff || ny > 65535) return ASTRA_ERR_SHAPE;
     const int lds = std::max(waves * Lds::all, waves * 256 * (int)sizeof(float));
@@ -472,21 +517,18 @@ static int launch_w4_wide(const W4Params& p, hipStream_t s) {
     return launch_w4_wide<TT, WR, WK, RT, 7>(p, s);
 }
 
-template <int TT>
 static int launch_w4_wide(const W4Params& p, hipStream_t s) {
-    // tiles of 128 rows where those are enough for the units, of 32 otherwise
-    if (ceil_div(p.N, 128) * ceil_div(p.n_tokens, 16 * TT) >= 192) return launch_w4_wide<TT, 4, 2, 2>(p, s);
-    return launch_w4_wide<TT, 2, 4, 1>(p, s);
+    // tiles of 128 rows where those are enough for the units; of 32, for 32 tokens, otherwise
+    if (p.n_tokens > 32 && ceil_div(p.N, 128) * ceil_div(p.n_tokens, 64) >= 192) return launch_w4_wide<4, 4, 2, 2>(p, s);
+    if (ceil_div(p.N, 128) * ceil_div(p.n_tokens, 32) >= 192) return launch_w4_wide<2, 4, 2, 2>(p, s);
+    return launch_w4_wide<2, 2, 4, 1>(p, s);
 }
 
 template <typename T>
 static int launch_w4(const W4Params& p, hipStream_t s) {
     if (p.n_tokens <= 2) return launch_w4<T, 2>(p, s);
     if (p.n_tokens <= 8) return launch_w4<T, 8>(p, s);
-    if constexpr (sizeof(T) == 2) {
-        if (p.n_tokens > 32) return launch_w4_wide<4>(p, s);
-        if (p.n_tokens > 16) return launch_w4_wide<2>(p, s);
-    }
+    if (sizeof(T) == 2 && p.n_tokens > 16) return launch_w4_wide(p, s);
     return launch_w4<T, 16>(p, s);
 }
 

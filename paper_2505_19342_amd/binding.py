@@ -330,74 +330,78 @@ def astra_decode_attention_static(desc: DecodeDesc, q, k_cache, v_cache, codes_k
                                                 _ptr(lse_out), _stream()), "astra_decode_attention_static")
 
 
-def _array(t, dtypes, n: int, device: int, what: str, strided: bool = False):
-    """Device address of an array of at least n elements on the current device; strided: a view whose rows may lie apart."""
-    if t is None:
-        return None
+def _array(t, dtype, n: int, device: int, what: str):
+    """Device address of a contiguous array of at least n elements on the current device."""
+    if t.dtype is dtype and t.numel() >= n and t.is_contiguous() and t.get_device() == device:
+        return t.data_ptr()
     if not t.is_cuda or t.get_device() != device:
         raise AstraError(f"{what}: a tensor on the current device required")
-    if t.dtype not in dtypes:
-        raise AstraError(f"{what}: element type {t.dtype}, one of {dtypes} required")
+    if t.dtype is not dtype:
+        raise AstraError(f"{what}: element type {t.dtype}, {dtype} required")
     if t.numel() < n:
         raise AstraError(f"{what}: {t.numel()} elements, {n} required")
-    if not strided and not t.is_contiguous():
-        raise AstraError(f"{what}: contiguous tensor required")
-    return t.data_ptr()
+    raise AstraError(f"{what}: contiguous tensor required")
 
 
 _types = None
 
 
 def _dtypes():
-    """element types by ASTRA_F32 / ASTRA_BF16, whole numbers, codes, fp32, and the function that tells the current device"""
+    """element types by ASTRA_F32 / ASTRA_BF16, int32, uint8, e4m3, and the functions that tell the current device and its stream"""
     global _types
     if _types is None:
         import torch
-        _types = (((torch.float32,), (torch.bfloat16,)), (torch.int32,), (torch.uint8, getattr(torch, "float8_e4m3fn", torch.uint8)), (torch.float32,),
-                  torch._C._cuda_getDevice)
+        _types = ((torch.float32, torch.bfloat16), torch.int32, torch.uint8, torch.float8_e4m3fn, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
     return _types
 
 
-def _rows(t, n: int, row: int, stride: int, types, device: int, what: str):
+def _rows(t, n: int, row: int, stride: int, dtype, device: int, what: str):
     """Address of n rows of `row` elements that lie `stride` (0: row) elements apart: a contiguous tensor that holds them, or a view whose first
     stride is that and whose rows are dense."""
-    if t is None:
-        return None
-    a = _array(t, types, n * row, device, what, strided=True)
-    if stride in (0, row):
-        if not t.is_contiguous():
-            raise AstraError(f"{what}: dense rows required; give the row stride in the descriptor")
-        return a
+    if stride == 0 or stride == row:
+        return _array(t, dtype, n * row, device, what)
     if t.is_contiguous():
-        fits = t.numel() >= (n - 1) * stride + row
-    else:
-        fits = t.dim() >= 2 and t.shape[0] >= n and t.stride(0) == stride and t[0].is_contiguous()
-    if not fits:
-        raise AstraError(f"{what}: rows of {row} elements, {stride} apart, required")
-    return a
+        return _array(t, dtype, (n - 1) * stride + row, device, what)
+    if not t.is_cuda or t.get_device() != device or t.dtype is not dtype:
+        raise AstraError(f"{what}: a tensor of {dtype} on the current device required")
+    if t.dim() < 2 or t.shape[0] < n or t.stride(0) != stride or t[0].numel() < row or not t[0].is_contiguous():
+        raise AstraError(f"{what}: {n} rows of {row} elements, {stride} apart, required")
+    return t.data_ptr()
 
 
-def _cache_arrays(d: CacheDesc, page_table, lens, first_row, k_pages, v_pages, k_scales, v_scales, ints, codes, f32, dev):
-    stride = d.table_stride or d.max_pages
-    blocks = d.n_pages * d.n_kv_heads
+def _elements(index: int, what: str):
+    if index not in (ASTRA_F32, ASTRA_BF16):
+        raise AstraError(f"{what}: {load().astra_status_string(-3).decode()} (-3)")
+    return _dtypes()[0][index]
+
+
+def _cache_arrays(d: CacheDesc, page_table, lens, first_row, k_pages, v_pages, k_scales, v_scales, device: int):
+    (f32, _), i32, u8, e4m3, _, _ = _types
+    seqs, heads = d.n_seqs, d.n_kv_heads
+    blocks = d.n_pages * heads
     values = blocks * d.page_size * d.head_dim
-    return (_array(page_table, ints, max(d.n_seqs - 1, 0) * stride + (d.max_pages if d.n_seqs > 0 else 0), dev, "page_table"), _array(lens, ints, d.n_seqs, dev, "lens"),
-            _array(first_row, ints, d.n_seqs + 1, dev, "first_row"), _array(k_pages, codes, values, dev, "k_pages"),
-            _array(v_pages, codes, values, dev, "v_pages"), _array(k_scales, f32, blocks, dev, "k_scales"), _array(v_scales, f32, blocks, dev, "v_scales"))
+    return (_array(page_table, i32, (seqs - 1) * (d.table_stride or d.max_pages) + d.max_pages if seqs > 0 else 0, device, "page_table"),
+            _array(lens, i32, seqs, device, "lens"), _array(first_row, i32, seqs + 1, device, "first_row"),
+            _array(k_pages, e4m3 if k_pages.dtype is e4m3 else u8, values, device, "k_pages"),
+            _array(v_pages, e4m3 if v_pages.dtype is e4m3 else u8, values, device, "v_pages"),
+            _array(k_scales, f32, blocks, device, "k_scales"), _array(v_scales, f32, blocks, device, "v_scales"))
 
 
 def astra_cache_append(desc: CacheDesc, page_table, lens, first_row, pos_shift, q, k, v, q_out, k_pages, v_pages, k_scales, v_scales):
     """page_table, lens, first_row, pos_shift: int32; k_pages, v_pages: uint8 or float8_e4m3fn.  q, k, v, q_out may be views of wider rows
-    (desc.q_stride, k_stride, v_stride)."""
-    elem, ints, codes, f32, device = _dtypes()
-    dev, dh = device(), desc.head_dim
-    x = elem[desc.dtype] if desc.dtype in (0, 1) else ()
-    table, le, first, kp, vp, ks, vs = _cache_arrays(desc, page_table, lens, first_row, k_pages, v_pages, k_scales, v_scales, ints, codes, f32, dev)
-    _check(load().astra_cache_append(
-        ctypes.byref(desc), table, le, first, _array(pos_shift, ints, desc.n_seqs, dev, "pos_shift"),
-        _rows(q, desc.n_tokens, desc.n_q_heads * dh, desc.q_stride, x, dev, "q"), _rows(k, desc.n_tokens, desc.n_kv_heads * dh, desc.k_stride, x, dev, "k"),
-        _rows(v, desc.n_tokens, desc.n_kv_heads * dh, desc.v_stride, x, dev, "v"), _rows(q_out, desc.n_tokens, desc.n_q_heads * dh, desc.q_stride, x, dev, "q_out"),
-        kp, vp, ks, vs, _stream()), "astra_cache_append")
+    (desc.q_stride, k_stride, v_stride); pos_shift may be None, and q with q_out."""
+    x = _elements(desc.dtype, "astra_cache_append")
+    dev = _types[4]()
+    n, dh = desc.n_tokens, desc.head_dim
+    wide, narrow = desc.n_q_heads * dh, desc.n_kv_heads * dh
+    table, le, first, kp, vp, ks, vs = _cache_arrays(desc, page_table, lens, first_row, k_pages, v_pages, k_scales, v_scales, dev)
+    rc = load().astra_cache_append(
+        ctypes.byref(desc), table, le, first, None if pos_shift is None else _array(pos_shift, _types[1], desc.n_seqs, dev, "pos_shift"),
+        None if q is None else _rows(q, n, wide, desc.q_stride, x, dev, "q"), _rows(k, n, narrow, desc.k_stride, x, dev, "k"),
+        _rows(v, n, narrow, desc.v_stride, x, dev, "v"), None if q_out is None else _rows(q_out, n, wide, desc.q_stride, x, dev, "q_out"),
+        kp, vp, ks, vs, _types[5](dev))
+    if rc:
+        _check(rc, "astra_cache_append")
 
 
 def astra_cache_attention_workspace_bytes(desc: CacheDesc) -> int:
@@ -406,28 +410,32 @@ def astra_cache_attention_workspace_bytes(desc: CacheDesc) -> int:
 
 def astra_cache_attention(desc: CacheDesc, page_table, lens, first_row, q, k_pages, v_pages, k_scales, v_scales, prior_out, prior_lse, out,
                           lse_out, workspace):
-    """Arguments as for astra_cache_append; prior_out, prior_lse and lse_out may be None."""
-    elem, ints, codes, f32, device = _dtypes()
-    dev, n = device(), desc.n_tokens * desc.n_q_heads
-    x = elem[desc.dtype] if desc.dtype in (0, 1) else ()
-    table, le, first, kp, vp, ks, vs = _cache_arrays(desc, page_table, lens, first_row, k_pages, v_pages, k_scales, v_scales, ints, codes, f32, dev)
-    _check(load().astra_cache_attention(
-        ctypes.byref(desc), table, le, first, _rows(q, desc.n_tokens, desc.n_q_heads * desc.head_dim, desc.q_stride, x, dev, "q"), kp, vp, ks, vs,
-        _array(prior_out, x, n * desc.head_dim, dev, "prior_out"), _array(prior_lse, f32, n, dev, "prior_lse"), _array(out, x, n * desc.head_dim, dev, "out"),
-        _array(lse_out, f32, n, dev, "lse_out"), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream()), "astra_cache_attention")
+    """Arguments as for astra_cache_append; prior_out with prior_lse, and lse_out, may be None."""
+    x = _elements(desc.dtype, "astra_cache_attention")
+    f32, dev = _types[0][0], _types[4]()
+    n, dh = desc.n_tokens * desc.n_q_heads, desc.head_dim
+    table, le, first, kp, vp, ks, vs = _cache_arrays(desc, page_table, lens, first_row, k_pages, v_pages, k_scales, v_scales, dev)
+    rc = load().astra_cache_attention(
+        ctypes.byref(desc), table, le, first, _rows(q, desc.n_tokens, desc.n_q_heads * dh, desc.q_stride, x, dev, "q"), kp, vp, ks, vs,
+        None if prior_out is None else _array(prior_out, x, n * dh, dev, "prior_out"), None if prior_lse is None else _array(prior_lse, f32, n, dev, "prior_lse"),
+        _array(out, x, n * dh, dev, "out"), None if lse_out is None else _array(lse_out, f32, n, dev, "lse_out"),
+        _array(workspace, workspace.dtype, 0, dev, "workspace"), workspace.numel() * workspace.element_size(), _types[5](dev))
+    if rc:
+        _check(rc, "astra_cache_attention")
 
 
 def astra_w4_linear(desc: W4Desc, x, n_tokens: int, codes, scales, zeros, bias, y):
     """codes, zeros: uint8 (see quantize_w4); zeros and bias may be None."""
-    elem, _, _, _, device = _dtypes()
-    dev, n_in, n_out = device(), desc.in_features, desc.out_features
-    xt, yt = (elem[i] if i in (0, 1) else () for i in (desc.dtype, desc.y_dtype))
+    xt, yt = _elements(desc.dtype, "astra_w4_linear"), _elements(desc.y_dtype, "astra_w4_linear")
+    u8, dev = _types[2], _types[4]()
+    n_in, n_out = desc.in_features, desc.out_features
     groups = n_out * (n_in // desc.group) if desc.group > 0 else 0
-    u8 = _types[2][:1]
-    _check(load().astra_w4_linear(
+    rc = load().astra_w4_linear(
         ctypes.byref(desc), _rows(x, n_tokens, n_in, desc.x_stride, xt, dev, "x"), n_tokens, _array(codes, u8, n_out * n_in // 2, dev, "codes"),
-        _array(scales, xt, groups, dev, "scales"), _array(zeros, u8, groups, dev, "zeros"), _array(bias, xt, n_out, dev, "bias"),
-        _array(y, yt, n_tokens * n_out, dev, "y"), _stream()), "astra_w4_linear")
+        _array(scales, xt, groups, dev, "scales"), None if zeros is None else _array(zeros, u8, groups, dev, "zeros"),
+        None if bias is None else _array(bias, xt, n_out, dev, "bias"), _array(y, yt, n_tokens * n_out, dev, "y"), _types[5](dev))
+    if rc:
+        _check(rc, "astra_w4_linear")
 
 
 def quantize_w4(w, group: int, dtype: str = "bf16", zeros: bool = False):

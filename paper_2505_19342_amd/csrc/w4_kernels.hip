@@ -95,6 +95,16 @@ struct Tokens<float> {
         }
     }
 };
+// the four lanes of a row each have one value: all four to all of them
+__device__ __forceinline__ void spread(uint32_t v, uint32_t (&out)[4]) {
+    const auto h = __builtin_amdgcn_permlane32_swap(v, v, false, false);        // lanes 0 .. 31 twice, lanes 32 .. 63 twice
+    const auto a = __builtin_amdgcn_permlane16_swap(h[0], h[0], false, false), b = __builtin_amdgcn_permlane16_swap(h[1], h[1], false, false);
+    out[0] = a[0];
+    out[1] = a[1];
+    out[2] = b[0];
+    out[3] = b[1];
+}
+
 // an element as it lies in memory, converted where it is used: a conversion beside the load is a wait there
 template <typename T>
 __device__ __forceinline__ uint32_t raw_element(const void* p, int64_t i) {
@@ -136,13 +146,11 @@ __device__ __forceinline__ void store_sums(const W4Params& p, float* sums, int w
 
 // Scales and zero points of 16 rows for 16 neighbouring groups, on their way through a wavefront's part of LDS: sixteen lanes load the sixteen of a row (a lane per row and
 // group would reach sixty-four places at a time), and each lane reads those of its row where a group ends.
-template <typename T>
 struct ScaleSpan {
     static constexpr int kGroups = 16;
-    using Raw = std::conditional_t<sizeof(T) == 2, uint16_t, uint32_t>;
-    static constexpr int kStride = sizeof(T) == 2 ? 18 : 17, kZeroStride = 20;      // rows start in different banks
-    static constexpr int kScaleBytes = 16 * kStride * (int)sizeof(Raw), kBytes = (kScaleBytes + 16 * kZeroStride + 15) / 16 * 16;
-    Raw s[4];
+    static constexpr int kStride = 18, kZeroStride = 20;      // rows start in different banks
+    static constexpr int kScaleBytes = 16 * kStride * 2, kBytes = (kScaleBytes + 16 * kZeroStride + 15) / 16 * 16;
+    uint16_t s[4];
     uint8_t z[4];
     // rows n0 .. n0 + 15 (those beyond the last: the last), groups from `first` on (beyond the last: the last)
     __device__ __forceinline__ void load(const W4Params& p, int n0, int groups, int first) {
@@ -150,7 +158,7 @@ struct ScaleSpan {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int64_t j = (int64_t)min(n0 + 4 * i + (lane >> 4), p.N - 1) * groups + at;
-            s[i] = ((const Raw*)p.scales)[j];
+            s[i] = ((const uint16_t*)p.scales)[j];
             if (p.zeros) z[i] = p.zeros[j];
         }
     }
@@ -158,12 +166,12 @@ struct ScaleSpan {
         const int lane = lane_id();
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            ((Raw*)lds)[(4 * i + (lane >> 4)) * kStride + (lane & 15)] = s[i];
+            ((uint16_t*)lds)[(4 * i + (lane >> 4)) * kStride + (lane & 15)] = s[i];
             if (p.zeros) ((uint8_t*)lds + kScaleBytes)[(4 * i + (lane >> 4)) * kZeroStride + (lane & 15)] = z[i];
         }
     }
     // of row lane % 16
-    __device__ __forceinline__ static float scale(const char* lds, int group) { return from_raw<T>(((const Raw*)lds)[(lane_id() & 15) * kStride + group]); }
+    __device__ __forceinline__ static float scale(const char* lds, int group) { return bf16_bits_to_f32(((const uint16_t*)lds)[(lane_id() & 15) * kStride + group]); }
     __device__ __forceinline__ static float zero(const W4Params& p, const char* lds, int group) {
         return p.zeros ? (float)(((const uint8_t*)lds + kScaleBytes)[(lane_id() & 15) * kZeroStride + group] & 15) : 8.f;
     }
@@ -173,18 +181,16 @@ constexpr int kW4RowBytes = 80;                    // of a row's 64 bytes in LDS
 template <typename T, int TP, int U>
 struct W4Lds {                                     // of a wavefront
     static constexpr int x_stride = U * 256 + 16;  // bytes of a token's part: sixteen tokens' pieces of one column fall into different banks
-    static constexpr int x_bytes = Tokens<T>::kParts * TP * x_stride, w_bytes = U * 16 * kW4RowBytes, all = x_bytes + w_bytes + ScaleSpan<T>::kBytes;
+    static constexpr int x_bytes = Tokens<T>::kParts * TP * x_stride, w_bytes = U * 16 * kW4RowBytes, all = x_bytes + w_bytes;
 };
 
-// Few tokens: a workgroup has 16 rows of the weights and TP <= 16 tokens, each of its wavefronts a range of columns; it takes U neighbouring blocks of 128 at a time, and a
-// batch's loads are on their way while the one before is worked on.  GS: log2 of the group; blockIdx.y: tile of 16 tokens
-template <int TP, int GS>
-constexpr int kW4MaxWaves = TP > 8 || GS == 5 ? 8 : 16;      // what registers leave room for
+// Few tokens: a workgroup has 16 rows of the weights and TP <= 16 tokens, its wavefronts take U neighbouring blocks of 128 columns in turn; a batch's loads are on
+// their way while the one before is worked on.  GS: log2 of the group; blockIdx.y: tile of 16 tokens
 template <typename T, int TP, int GS, int U>
-__global__ __launch_bounds__((kW4MaxWaves<TP, GS> * kWave)) void w4_kernel(const W4Params p) {
+__global__ __launch_bounds__(1024) void w4_kernel(const W4Params p) {
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int PARTS = Tokens<T>::kParts, NG = 128 >> GS, STEPS = 4 / NG;      // groups in a block, products of 32 columns in a group
-    constexpr int GROUPS = U * NG, PER_SPAN = ScaleSpan<T>::kGroups / GROUPS;       // groups in a batch, batches whose scales are brought together
+    constexpr int GROUPS = U * NG, NS = (GROUPS + 3) / 4;                         // groups in a batch, loads for their scales
     constexpr int PIECES = U * 16, NX = (TP * PIECES + 63) / 64;                  // pieces of eight columns of a token in a batch, and of a lane
     using Lds = W4Lds<T, TP, U>;
     extern __shared__ __align__(16) char w4_lds[];
@@ -196,13 +202,15 @@ __global__ __launch_bounds__((kW4MaxWaves<TP, GS> * kWave)) void w4_kernel(const
     const int groups = p.K >> GS, batches = (p.K + 128 * U - 1) / (128 * U);
     char* const lds_x = w4_lds + wave * Lds::all;
     char* const lds_w = lds_x + Lds::x_bytes;
-    char* const lds_s = lds_w + Lds::w_bytes;
 
-    // what this lane loads: a piece of a row (row lane / 4), pieces of tokens: offsets from what the workgroup has first
+    // what this lane loads: a piece of a row (row lane / 4), the scale of group g of a row (row lane % 16), pieces of tokens: offsets from what the workgroup has first
     const uint8_t* const codes = p.codes + (int64_t)n0 * (p.K >> 1);
+    const char* const scales = (const char*)p.scales + (int64_t)n0 * groups * (int)sizeof(T);
+    const uint8_t* const zeros = p.zeros + (int64_t)n0 * groups;
     const char* const x = (const char*)p.x + t0 * p.x_stride * (int)sizeof(T);
     const int last_row = p.N - 1 - n0;
     const uint32_t w_at = (uint32_t)min(lane >> 2, last_row) * (uint32_t)(p.K >> 1) + 16u * (lane & 3);
+    const uint32_t group_at = (uint32_t)min(col, last_row) * (uint32_t)groups;
     uint32_t x_at[NX];
 #pragma unroll
     for (int i = 0; i < NX; ++i) {
@@ -211,7 +219,7 @@ __global__ __launch_bounds__((kW4MaxWaves<TP, GS> * kWave)) void w4_kernel(const
     }
 
     u32x4 raw_w[U];
-    ScaleSpan<T> span;
+    uint32_t raw_scale[NS], raw_zero[NS];
     Tokens<T> raw_x[NX];
     auto load = [&](int batch) __attribute__((always_inline)) {
         const int k0 = batch * 128 * U;
@@ -226,6 +234,12 @@ __global__ __launch_bounds__((kW4MaxWaves<TP, GS> * kWave)) void w4_kernel(const
             raw_w[u] = *reinterpret_cast<const u32x4*>(wk + (all ? (int64_t)at : (int64_t)(int)at));
         }
 #pragma unroll
+        for (int i = 0; i < NS; ++i) {
+            const uint32_t at = group_at + (uint32_t)min((k0 >> GS) + 4 * i + g, groups - 1);
+            raw_scale[i] = raw_element<T>(scales, at);
+            if (p.zeros) raw_zero[i] = zeros[at];
+        }
+#pragma unroll
         for (int i = 0; i < NX; ++i) {
             int back = 0;
             if (!all) back = max(8 * ((i * 64 + lane) % PIECES) - (p.K - 8 - k0), 0) * (int)sizeof(T);
@@ -235,17 +249,9 @@ __global__ __launch_bounds__((kW4MaxWaves<TP, GS> * kWave)) void w4_kernel(const
     const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
     const OffsetConstants constants;
     f32x4 acc[1][1] = {};
-    const int per_wave = (batches + waves - 1) / waves, begin = min(wave * per_wave, batches), end = min(begin + per_wave, batches);
-    if (begin < end) {
-        span.load(p, n0, groups, begin * GROUPS);
-        load(begin);
-    }
-    for (int batch = begin; batch < end; ++batch) {
-        const int in_span = (batch - begin) % PER_SPAN;
-        if (in_span == 0) {
-            span.put(p, lds_s);
-            if (batch + PER_SPAN < end) span.load(p, n0, groups, (batch + PER_SPAN) * GROUPS);
-        }
+    int batch = wave;
+    if (batch < batches) load(batch);
+    while (batch < batches) {
         // to LDS, a wavefront's own part: its reads come after its writes, nobody else is waited for
 #pragma unroll
         for (int u = 0; u < U; ++u) *reinterpret_cast<u32x4*>(lds_w + (u * 16 + (lane >> 2)) * kW4RowBytes + 16 * (lane & 3)) = raw_w[u];
@@ -258,7 +264,21 @@ __global__ __launch_bounds__((kW4MaxWaves<TP, GS> * kWave)) void w4_kernel(const
 #pragma unroll
                 for (int k = 0; k < PARTS; ++k) *reinterpret_cast<u32x4*>(lds_x + (k * TP + token) * Lds::x_stride + 16 * piece) = a[k];
         }
-        if (batch + 1 < end) load(batch + 1);
+        float scale[NS][4], zero[NS][4];
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+            uint32_t s[4], z[4];
+            spread((batch * 128 * U >> GS) + 4 * i + g < groups ? raw_scale[i] : 0u, s);
+            if (p.zeros) spread(raw_zero[i], z);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float sc = from_raw<T>(s[j]), zr = p.zeros ? (float)(z[j] & 15u) : 8.f;
+                scale[i][j] = F32 ? 16.f * sc : sc;
+                zero[i][j] = F32 ? (zr - 8.f) * 0.0625f : zr + kOffset;
+            }
+        }
+        const int next = batch + waves;
+        if (next < batches) load(next);
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -276,14 +296,11 @@ __global__ __launch_bounds__((kW4MaxWaves<TP, GS> * kWave)) void w4_kernel(const
                         if (!F32 || p.zeros) sum = mfma_16x16x32(xa, ones, sum);
                     }
                 }
-                const int in = in_span * GROUPS + u * NG + j;
-                const float zr = ScaleSpan<T>::zero(p, lds_s, in);
-                float sc = ScaleSpan<T>::scale(lds_s, in);
-                if (batch * GROUPS + u * NG + j >= groups) sc = 0.f;
-                const float s = F32 ? 16.f * sc : sc, z = F32 ? (zr - 8.f) * 0.0625f : zr + kOffset;
+                const int i = (u * NG + j) >> 2, jj = (u * NG + j) & 3;
 #pragma unroll
-                for (int v = 0; v < 4; ++v) acc[0][0][v] = fmaf(s, fmaf(-z, sum[v], d[v]), acc[0][0][v]);
+                for (int v = 0; v < 4; ++v) acc[0][0][v] = fmaf(scale[i][jj], fmaf(-zero[i][jj], sum[v], d[v]), acc[0][0][v]);
             }
+        batch = next;
     }
     __syncthreads();                               // everybody is through with its part of LDS
     store_sums<T, 1, 1>(p, (float*)w4_lds, wave, waves, t0, n0, acc);
@@ -299,7 +316,7 @@ struct W4Wide {
     static constexpr int x_bytes = TT * 4 * 1024;                               // [tile][32 columns][lane of the operand] 16 bytes
     static constexpr int sum_bytes = (128 >> GS) * TT * 16 * 4;                 // [group][token]
     static constexpr int of_group = x_bytes + sum_bytes;
-    static constexpr int w_bytes = RT * 16 * kW4RowBytes, span_bytes = RT * ScaleSpan<uint16_t>::kBytes;
+    static constexpr int w_bytes = RT * 16 * kW4RowBytes, span_bytes = RT * ScaleSpan::kBytes;
     static constexpr int all = 2 * WK * of_group + waves * (2 * w_bytes + span_bytes);
     static constexpr int lds = all > waves * RT * 1024 ? all : waves * RT * 1024;
     static_assert(lds <= 160 * 1024, "LDS of a unit");
@@ -325,7 +342,7 @@ __device__ __forceinline__ float add_dpp(float v) {
 template <int TT, int WR, int WK, int RT, int GS>
 __global__ __launch_bounds__((W4Wide<TT, WR, WK, RT, GS>::threads), 2) void w4_wide_kernel(const W4Params p) {
     using Shape = W4Wide<TT, WR, WK, RT, GS>;
-    using Span = ScaleSpan<uint16_t>;
+    using Span = ScaleSpan;
     constexpr int NG = 128 >> GS, STEPS = 4 / NG, PER_SPAN = Span::kGroups / NG;
     constexpr int LANES = WR * kWave;                                            // of a group of wavefronts
     constexpr int NX = TT * 16 * 16 / LANES;                                     // pieces of eight columns of a token that a lane brings to LDS
@@ -399,9 +416,9 @@ __global__ __launch_bounds__((W4Wide<TT, WR, WK, RT, GS>::threads), 2) void w4_w
         }
         const char* const x = lds_x + half * Shape::of_group;
         const char* const w = lds_w + half * Shape::w_bytes;
-#pragma unroll
+        constexpr int kAtOnce = TT * RT * NG > 16 ? 1 : NG;    // groups whose operands there are registers for
+#pragma unroll kAtOnce
         for (int j = 0; j < NG; ++j) {
-            __builtin_amdgcn_sched_barrier(0);             // one group's operands at a time: registers
             f32x4 d[TT][RT] = {};
 #pragma unroll
             for (int a = j * STEPS; a < (j + 1) * STEPS; ++a) {
@@ -476,7 +493,7 @@ template <typename T, int TP, int GS, int U>
 static int launch_w4(const W4Params& p, hipStream_t s) {
     static std::atomic<uint64_t> allowed{0};
     using Lds = W4Lds<T, TP, U>;
-    const int batches = (int)ceil_div(p.K, 128 * U), most = kW4MaxWaves<TP, GS>, waves = batches < most ? batches : most;
+    const int batches = (int)ceil_div(p.K, 128 * U), most = TP > 8 ? 8 : 16, waves = batches < most ? batches : most;
     const int64_t nx = ceil_div(p.N, 16), ny = ceil_div(p.n_tokens, 16);
     if (nx > 0x7fffffff || ny > 65535) return ASTRA_ERR_SHAPE;
     const int lds = std::max(waves * Lds::all, waves * 256 * (int)sizeof(float));

@@ -347,9 +347,12 @@ struct CacheWalk {
 // a workgroup has at most two such pieces, one that ends a row block begun by others (slot 2w) and one that begins one (slot 2w + 1).
 // The workgroup that begins a block notes how many pieces there are, and a second launch joins them in order.
 // Where sequences cannot be long (CUT = false), a row block is one unit, the workgroups have more wavefronts and there is no second launch.
-constexpr int kCaMinShare = 8;        // tiles
+constexpr int kCaMinShare = 2;        // tiles; 8 where there are enough for every unit: fewer pieces to join (313 tiles of 8 row blocks: 14.3 us, 16.5 with shares of 4)
 constexpr int kCaCus = 256;
-constexpr int kCaMaxTiles = 64;       // of a sequence that is not cut
+// Tiles of a sequence that is not cut.  A row block that one workgroup walks takes about 5 us and 0.3 us a tile, one after the other where there are more than units; cut ones
+// take 11 us with their join and 1.7 ns a tile of them all (heads of 128).  8 row blocks of 33 tiles: 14.3 us whole, 12.4 cut, of 62: 16.2 and 11.4; 64 of up to 64: 18.3 and 18.0;
+// 512 of up to 64: 38 and 49, of up to 125: 60 and 66.  Only the capacity is known here: beyond 128 a sequence is cut whatever there is beside it, or one long one would hold up the others.
+static int cache_attn_whole_tiles(int64_t blocks) { return blocks < 24 ? 24 : blocks < 128 ? (int)blocks : 128; }
 
 // how many wavefronts a workgroup has and how many workgroups the registers of a unit leave room for
 template <int DH, typename T, int NT, bool CUT>
@@ -464,7 +467,7 @@ __global__ __launch_bounds__((CaShape<DH, T, NT, CUT>::threads), (CaShape<DH, T,
         __syncthreads();
         all = before[c.n_seqs];
     }
-    const uint32_t share = CUT ? max((all + gridDim.x - 1) / gridDim.x, (uint32_t)kCaMinShare) : 1u;
+    const uint32_t share = CUT ? max((all + gridDim.x - 1) / gridDim.x, min(max(all / kCaCus, (uint32_t)kCaMinShare), 4u * kCaMinShare)) : 1u;
     uint32_t u = blockIdx.x < (all + share - 1) / share ? blockIdx.x * share : all;
     const uint32_t end = all - u < share ? all : u + share;
     CaJoin join = {};
@@ -695,7 +698,7 @@ static int cache_attn_plan(const astra_cache_desc& d, CacheAttnPlan* pl) {
     const int64_t tiles = ceil_div((int64_t)d.max_pages * d.page_size, kCaTile);
     const int64_t blocks = (rows / (16 * s.nt) + d.n_seqs) * d.n_kv_heads;               // no more than these
     if (rows > (1 << 30) || blocks * tiles > 0x7fffffff) return ASTRA_ERR_UNSUPPORTED;   // rows and units are counted in 32 bits
-    s.cut = tiles > kCaMaxTiles;
+    s.cut = tiles > cache_attn_whole_tiles(blocks);
     s.wgs = (int)blocks;
     if (s.cut) {
         int most = d.head_dim == 64    ? f32 ? cache_attn_wgs<64, float>(s.nt) : cache_attn_wgs<64, uint16_t>(s.nt)

@@ -83,7 +83,8 @@ struct RowBlock {
 // NT: groups of 16 query rows
 template <int DH, typename T, int NT>
 struct CacheWalk {
-    static constexpr int KJ = DH / 64;         // 16-byte pieces of a key row per lane
+    static constexpr int KR = DH < 128 ? DH : 128;                  // bytes of a key row that are in LDS at a time
+    static constexpr int KP = KR / 16, KN = 32 * KR / 1024;         // 16-byte pieces of it, and a lane's of the tile
     static constexpr int KC = DH / 32;         // contraction steps of a score
     static constexpr int VCH = DH / 16;        // value channels per lane
     static constexpr bool F32 = sizeof(T) == 4;
@@ -92,7 +93,7 @@ struct CacheWalk {
 
     // a tile's codes and the scales of its two 16-token halves
     struct Keys {
-        u32x4 k[2][KJ];
+        u32x4 k[DH / KR][KN];
         float scale[2];
     };
     struct Values {
@@ -170,14 +171,17 @@ struct CacheWalk {
         return ((block << p.c.page_shift) + ((t * kCaTile + 16 * hf) & ((1 << p.c.page_shift) - 1))) * DH;
     }
     __device__ __forceinline__ static void load(const CacheAttnParams& p, const RowBlock& b, int t, const Pages& pg, Keys& x) {
-        const uint32_t lane_at = (uint32_t)(lane_id() & 15) * DH + (uint32_t)(lane_id() >> 4) * 16u;
+        // neighbouring lanes: neighbouring pieces of a row (one row per lane, as the operand has them, costs the first-level cache four times the cycles)
+        const uint32_t lane_at = (uint32_t)(lane_id() / KP) * DH + (uint32_t)(lane_id() % KP) * 16u;
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
             const int64_t block = pg.block(p.c, hf, b.kv_head);
             x.scale[hf] = ld_global<float>((gbytes)(p.k_scales + block));
             const gbytes kb = (gbytes)p.k_pages + half_at(p, block, t, hf);
 #pragma unroll
-            for (int j = 0; j < KJ; ++j) x.k[hf][j] = ld_global<u32x4>(kb + lane_at + 64 * j);
+            for (int c = 0; c < DH / KR; ++c)
+#pragma unroll
+                for (int i = 0; i < KN / 2; ++i) x.k[c][hf * (KN / 2) + i] = ld_global<u32x4>(kb + lane_at + i * (64 / KP) * DH + c * KR);
         }
     }
     __device__ __forceinline__ static void load(const CacheAttnParams& p, const RowBlock& b, int t, const Pages& pg, Values& x) {
@@ -198,25 +202,39 @@ struct CacheWalk {
     }
 
     // scores of a tile in base-2 units, not yet masked
-    __device__ __forceinline__ void score(const CacheAttnParams& p, const Keys& x, float (&s)[NT][8]) const {
+    // lds: 32 * KR bytes of the wavefront's own; its reads come after its writes, nobody else is waited for.  Pieces are exchanged within a row so that the
+    // sixteen rows of an operand's quarter fall into different banks.
+    __device__ __forceinline__ void score(const CacheAttnParams& p, const Keys& x, char* lds, float (&s)[NT][8]) const {
         const float sl2 = p.scale * kLog2e;
+        const int lane = lane_id(), col = lane & 15, g = lane >> 4;
+        auto slot = [](int row, int piece) __attribute__((always_inline)) { return row * KR + (piece ^ (KP == 8 ? (row >> 1) & 7 : (row >> 2) & 3)) * 16; };
+        f32x4 d[2][NT] = {};
+#pragma unroll
+        for (int c = 0; c < DH / KR; ++c) {
+#pragma unroll
+            for (int i = 0; i < KN; ++i) *reinterpret_cast<u32x4*>(lds + slot(i * (64 / KP) + lane / KP, lane % KP)) = x.k[c][i];
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+                for (int j = 0; j < KR / 64; ++j) {
+                    const u32x4 w = *reinterpret_cast<const u32x4*>(lds + slot(16 * hf + col, 4 * j + g));
+#pragma unroll
+                    for (int a = 0; a < 2; ++a) {
+                        const bf16x8 kf = a ? eight_codes(w.z, w.w) : eight_codes(w.x, w.y);
+#pragma unroll
+                        for (int i = 0; i < QP; ++i)
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) d[hf][n] = mfma_16x16x32(kf, q[n][i][(c * KR / 64 + j) * 2 + a], d[hf][n]);
+                    }
+                }
+        }
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
-            f32x4 d[NT] = {};
-#pragma unroll
-            for (int kc = 0; kc < KC; ++kc) {
-                const u32x4& w = x.k[hf][kc >> 1];
-                const bf16x8 kf = kc & 1 ? eight_codes(w.z, w.w) : eight_codes(w.x, w.y);
-#pragma unroll
-                for (int i = 0; i < QP; ++i)
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) d[n] = mfma_16x16x32(kf, q[n][i][kc], d[n]);
-            }
             const float f = sl2 * x.scale[hf];
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int v = 0; v < 4; ++v) s[n][4 * hf + v] = d[n][v] * f;
+                for (int v = 0; v < 4; ++v) s[n][4 * hf + v] = d[hf][n][v] * f;
         }
     }
 
@@ -425,7 +443,8 @@ __global__ __launch_bounds__((CaShape<DH, T, NT, CUT>::threads), (CaShape<DH, T,
     constexpr int PASS = 4, STRIDE = 16 * PASS + 4;               // channels per thread and pass when the wavefronts are joined
     __shared__ uint32_t before[kCacheMaxSeqs + 1];                // units before a sequence, where there are more than 64
     __shared__ float ml[WAVES][ROWS][2];
-    __shared__ __align__(16) float sums[WAVES][16][STRIDE];
+    __shared__ __align__(16) float sums[WAVES][16][STRIDE];       // of a wavefront; while it walks, a tile of keys on its way to the operand
+    static_assert(sizeof(sums[0]) >= 32 * Walk::KR, "a tile of keys");
     // the arguments arrive together; each use asking for its own is another trip to them
     asm volatile("" ::"s"(p.c.table), "s"(p.c.lens), "s"(p.c.first), "s"(p.q), "s"(p.k_pages), "s"(p.v_pages), "s"(p.k_scales), "s"(p.v_scales), "s"(p.c.n_seqs),
                  "s"(p.c.n_tokens), "s"(p.c.max_pages), "s"(p.c.table_stride), "s"(p.c.n_pages), "s"(p.c.page_shift), "s"(p.c.Hq), "s"(p.c.Hkv), "s"(p.q_stride),
@@ -527,7 +546,7 @@ __global__ __launch_bounds__((CaShape<DH, T, NT, CUT>::threads), (CaShape<DH, T,
             for (;;) {
                 const int then = min(t + WAVES, stop - 1);
                 float s[NT][8];
-                w.score(p, k, s);
+                w.score(p, k, reinterpret_cast<char*>(sums[wave]), s);
                 Walk::load(p, b, then, next, k);
                 w.absorb(p, b, t, now, s, v);
                 Walk::load(p, b, then, next, v);

@@ -360,7 +360,8 @@ struct CacheWalk {
 // ---- the work of a launch, dealt out --------------------------------------------------------------
 // A unit is a tile of 32 tokens for one row block.  The units of all row blocks (sequence by sequence, head by head, block by block of rows, the tiles of a
 // block in order) are cut into equal shares, one per workgroup: ragged batches keep every workgroup busy equally long, and one long context is
-// walked by all of them.  Only the device knows the lengths, so every workgroup adds them up itself.  The wavefronts take the tiles
+// walked by all of them.  Where there are at least four times as many workgroups as row blocks, a unit is `step` tiles, so many that a unit per workgroup is enough: a workgroup
+// that ends one block and begins another starts and joins its wavefronts twice (64 row blocks of up to 250 tiles: 36.7 us in equal shares, 21.6 so; 256 of up to 250: 53.6, 57.2).  Only the device knows the lengths, so every workgroup adds them up itself.  The wavefronts take the tiles
 // of a share in turn and are joined in LDS.  Where a share ends inside a row block, the unnormalised sums go to the scratch array:
 // a workgroup has at most two such pieces, one that ends a row block begun by others (slot 2w) and one that begins one (slot 2w + 1).
 // The workgroup that begins a block notes how many pieces there are, and a second launch joins them in order.
@@ -454,7 +455,6 @@ __global__ __launch_bounds__((CaShape<DH, T, NT, CUT>::threads), (CaShape<DH, T,
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int share_h = c.Hq / c.Hkv;
 
-    auto units = [&](const SequencePlan& sp) __attribute__((always_inline)) { return (CUT ? sp.tiles(c) : 1u) * sp.blocks(c, ROWS) * (uint32_t)c.Hkv; };
     auto scan = [&](uint32_t x) __attribute__((always_inline)) {       // sum of the lanes up to this one
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
@@ -464,11 +464,30 @@ __global__ __launch_bounds__((CaShape<DH, T, NT, CUT>::threads), (CaShape<DH, T,
         return x;
     };
     // up to 64 sequences: a lane has one of them
-    SequencePlan lane_plan(0, 0, 0);
-    uint32_t lane_before = 0, all;
     const bool few = c.n_seqs <= 64;
+    SequencePlan lane_plan(0, 0, 0);
+    if (few && lane < c.n_seqs) lane_plan = SequencePlan(c, lane);
+    uint32_t step = 1, share = 1;
+    if constexpr (CUT) {
+        uint32_t tiles = 0, blocks = 0;
+        auto count = [&](const SequencePlan& sp) __attribute__((always_inline)) {
+            const uint32_t b = sp.blocks(c, ROWS) * (uint32_t)c.Hkv;
+            blocks += b;
+            tiles += b * sp.tiles(c);
+        };
+        if (few) count(lane_plan);
+        else
+            for (int s = lane; s < c.n_seqs; s += 64) count(SequencePlan(c, s));
+        blocks = __builtin_amdgcn_readlane(scan(blocks), 63);
+        tiles = __builtin_amdgcn_readlane(scan(tiles), 63);
+        const uint32_t least = min(max(tiles / kCaCus, (uint32_t)kCaMinShare), 4u * kCaMinShare);
+        if (4 * blocks <= gridDim.x) step = max((tiles + gridDim.x - blocks - 1) / (gridDim.x - blocks), least);
+        else share = max((tiles + gridDim.x - 1) / gridDim.x, least);
+    }
+    auto per_block = [&](const SequencePlan& sp) __attribute__((always_inline)) { return CUT ? (sp.tiles(c) + step - 1) / step : 1u; };
+    auto units = [&](const SequencePlan& sp) __attribute__((always_inline)) { return per_block(sp) * sp.blocks(c, ROWS) * (uint32_t)c.Hkv; };
+    uint32_t lane_before = 0, all;
     if (few) {
-        if (lane < c.n_seqs) lane_plan = SequencePlan(c, lane);
         const uint32_t mine = lane < c.n_seqs ? units(lane_plan) : 0u, upto = scan(mine);
         lane_before = upto - mine;
         all = __builtin_amdgcn_readlane(upto, 63);
@@ -486,7 +505,6 @@ __global__ __launch_bounds__((CaShape<DH, T, NT, CUT>::threads), (CaShape<DH, T,
         __syncthreads();
         all = before[c.n_seqs];
     }
-    const uint32_t share = CUT ? max((all + gridDim.x - 1) / gridDim.x, min(max(all / kCaCus, (uint32_t)kCaMinShare), 4u * kCaMinShare)) : 1u;
     uint32_t u = blockIdx.x < (all + share - 1) / share ? blockIdx.x * share : all;
     const uint32_t end = all - u < share ? all : u + share;
     CaJoin join = {};
@@ -515,10 +533,11 @@ __global__ __launch_bounds__((CaShape<DH, T, NT, CUT>::threads), (CaShape<DH, T,
             in = u - before[s];
             sp = SequencePlan(c, s);
         }
-        const uint32_t all_tiles = sp.tiles(c), blocks = sp.blocks(c, ROWS), tiles = CUT ? all_tiles : 1u;
-        const uint32_t row = in / tiles;
-        const int tile0 = __builtin_amdgcn_readfirstlane((int)(in - row * tiles));
-        const int count = __builtin_amdgcn_readfirstlane((int)min(tiles - tile0, end - u));
+        const uint32_t all_tiles = sp.tiles(c), blocks = sp.blocks(c, ROWS), of_block = per_block(sp);
+        const uint32_t row = in / of_block;
+        const int unit0 = __builtin_amdgcn_readfirstlane((int)(in - row * of_block));
+        const int count = __builtin_amdgcn_readfirstlane((int)min(of_block - unit0, end - u));
+        const int tile0 = unit0 * (int)step;
         RowBlock b;
         b.seq = s;
         b.kv_head = __builtin_amdgcn_readfirstlane((int)(row / blocks));
@@ -533,7 +552,7 @@ __global__ __launch_bounds__((CaShape<DH, T, NT, CUT>::threads), (CaShape<DH, T,
         Walk w;
         // The next tile's keys are asked for as soon as this one's have become scores, its values once this one's are in the sums, the numbers of
         // its pages a tile earlier; beyond the last tile it is asked for again, so that there is one body and no wait covers more than it is for.
-        const int stop = min(CUT ? tile0 + count : (int)all_tiles, (b.all + kCaTile - 1) / kCaTile);
+        const int stop = min(CUT ? tile0 + count * (int)step : (int)all_tiles, (b.all + kCaTile - 1) / kCaTile);
         int t = tile0 + wave;
         if (t < stop) {
             typename Walk::Keys k;
@@ -568,8 +587,8 @@ __global__ __launch_bounds__((CaShape<DH, T, NT, CUT>::threads), (CaShape<DH, T,
                 ml[wave][16 * n + col][1] = w.l[n];
             }
         __syncthreads();
-        const bool whole = !CUT || count == (int)tiles;
-        const int64_t slot = 2 * (int64_t)blockIdx.x + (tile0 == 0 ? 1 : 0);
+        const bool whole = !CUT || count == (int)of_block;
+        const int64_t slot = 2 * (int64_t)blockIdx.x + (unit0 == 0 ? 1 : 0);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             float m = ml[0][16 * n + col][0];
@@ -616,7 +635,7 @@ __global__ __launch_bounds__((CaShape<DH, T, NT, CUT>::threads), (CaShape<DH, T,
                 }
             }
         }
-        if (!whole && tile0 == 0) join = CaJoin{(int)((u + tiles - 1) / share) - (int)blockIdx.x + 1, b.row0, b.n_rows, b.kv_head, b.from, {0, 0, 0}};      // up to the workgroup with the block's last tile
+        if (!whole && unit0 == 0) join = CaJoin{(int)((u + of_block - 1) / share) - (int)blockIdx.x + 1, b.row0, b.n_rows, b.kv_head, b.from, {0, 0, 0}};      // up to the workgroup with the block's last tile
         u += count;
         __syncthreads();                         // before the next block's sums
     }

@@ -561,6 +561,9 @@ __global__ __launch_bounds__((CaShape<DH, T, NT, CUT>::threads), (CaShape<DH, T,
             typename Walk::Pages next = Walk::pages(p, b, min(t + WAVES, stop - 1));
             w.start(p, b);
             Walk::load(p, b, t, now, k);
+            // Keys before values, as in the loop: a wait counts loads in their order, and the loop's first wait has to hold for either way into it.
+            // Left to the compiler the values came first here and every tile waited for all loads.
+            asm volatile("" ::: "memory");
             Walk::load(p, b, t, now, v);
             for (;;) {
                 const int then = min(t + WAVES, stop - 1);

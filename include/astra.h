@@ -319,7 +319,8 @@ int astra_decode_attention_static(const astra_decode_desc* desc, const void* q, 
  * Both calls of a step take the same descriptor, table, lens and first_row; the caller adds the new tokens to lens
  * afterwards.  Sequences may share pages that are full; a page that a call writes to belongs to one entry of one sequence.
  *   q                   rows of H_q * dh elements, q_stride elements apart; k, v: rows of H_kv * dh, k_stride, v_stride
- * Strides are whole multiples of 16 bytes.  head_dim 64, 128 or 256; page_size 16, 32, 64 or 128; at most 1024 sequences. */
+ * Strides are whole multiples of 16 bytes.  head_dim 64, 128 or 256; page_size 16, 32, 64 or 128; at most 1024
+ * sequences, 2^24 rows and 2^30 tokens of a sequence (sizes whose launch would pass 2^32 threads are unsupported, too). */
 typedef struct {
     int32_t dtype;              /* element type of q, k, v, prior_out, out */
     int32_t n_q_heads, n_kv_heads, head_dim;
@@ -370,8 +371,9 @@ int astra_cache_attention(const astra_cache_desc* desc, const int32_t* page_tabl
  *   zeros    nullable [out_features, in_features / group] bytes, 0 .. 15 (their lower four bits count); NULL means 8
  *   bias     nullable [out_features] in the element type
  *   y        [n_tokens, out_features], fp32 or bf16 (y_dtype)
- * group 32, 64 or 128, a divisor of in_features.  Sums are kept in fp32.  The kernel reads the weights once for every 64
- * tokens: many tokens are served correctly, but are the business of the layer's own products. */
+ * group 32, 64 or 128, a divisor of in_features; n_tokens at most 2^19, in_features and out_features 2^24, x_stride 2^25.
+ * Sums are kept in fp32.  The weights are read once for every 16 tokens in fp32, for every 32 or 64 in bf16: many tokens are
+ * served correctly, but are the business of the layer's own products. */
 typedef struct {
     int32_t dtype;              /* element type of x, scales, bias */
     int32_t y_dtype;

@@ -738,7 +738,8 @@ static int cache_attn_plan(const astra_cache_desc& d, CacheAttnPlan* pl) {
     s.nt = !f32 && d.head_dim <= 128 && rows >= 32 * (int64_t)d.n_seqs ? 2 : 1;
     const int64_t tiles = ceil_div((int64_t)d.max_pages * d.page_size, kCaTile);
     const int64_t blocks = (rows / (16 * s.nt) + d.n_seqs) * d.n_kv_heads;               // no more than these
-    if (rows > (1 << 30) || blocks * tiles > 0x7fffffff) return ASTRA_ERR_UNSUPPORTED;   // rows and units are counted in 32 bits
+    // rows and units are counted in 32 bits; workgroups have no more than 1024 threads
+    if (rows > (1 << 30) || blocks * tiles > 0x7fffffff || blocks * 1024 > kMaxGridThreads) return ASTRA_ERR_UNSUPPORTED;
     s.cut = tiles > cache_attn_whole_tiles(blocks);
     s.wgs = (int)blocks;
     if (s.cut) {

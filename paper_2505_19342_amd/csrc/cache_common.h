@@ -6,6 +6,7 @@ namespace astra {
 
 constexpr int kCacheMaxSeqs = 1024;
 constexpr float kE4m3Max = 448.f;
+constexpr int64_t kMaxGridThreads = 0xffffffff;      // of a launch, as the runtime takes it
 
 // The arrays and sizes of a step.  What they say is checked where it is used: no entry of the table, no length and no row number
 // takes an access out of its array.

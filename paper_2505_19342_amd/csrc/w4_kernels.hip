@@ -30,6 +30,7 @@ struct W4Params {
 
 __device__ __forceinline__ f32x4 mfma_16x16x32(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
+constexpr int kW4MaxTokens = 1 << 19;              // tiles of 16 fit the grid's second side
 constexpr float kOffset = 16.f;
 // Eight codes as 16 + code, in the order 0 4 1 5 2 6 3 7.  The constants are kept where one instruction can have both (as literals they are two).
 struct OffsetConstants {
@@ -119,28 +120,21 @@ __device__ __forceinline__ float element(const void* p, int64_t i) {
     else return ((const float*)p)[i];
 }
 
-// Sums of the wavefronts in order, and the store: tiles of 16 tokens one after the other.  The caller's rows are n0 .. n0 + 16 * RT - 1, its tokens t0 .. t0 + 16 * TT - 1;
-// sums: [wavefronts][16][16 * RT] floats
-template <typename T, int TT, int RT>
-__device__ __forceinline__ void store_sums(const W4Params& p, float* sums, int wave, int waves, int64_t t0, int n0, const f32x4 (&acc)[TT][RT]) {
+// Sums of the wavefronts in order, and the store: 16 rows of the weights, from n0 on, and 16 tokens, from t0 on; sums: [wavefronts][16][16] floats
+template <typename T>
+__device__ __forceinline__ void store_sums(const W4Params& p, float* sums, int wave, int waves, int64_t t0, int n0, f32x4 acc) {
     const int lane = lane_id(), col = lane & 15, g = lane >> 4;
 #pragma unroll
-    for (int i = 0; i < TT; ++i) {
-        if (i > 0) __syncthreads();
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) sums[((wave * 16 + 4 * g + v) * RT + r) * 16 + col] = acc[i][r][v];
-        __syncthreads();
-        for (int e = threadIdx.x; e < 256 * RT; e += blockDim.x) {
-            const int64_t t = t0 + 16 * i + e / (16 * RT);
-            const int n = n0 + e % (16 * RT);
-            if (t >= p.n_tokens || n >= p.N) continue;
-            float y = p.bias ? element<T>(p.bias, n) : 0.f;
-            for (int k = 0; k < waves; ++k) y += sums[k * 256 * RT + e];
-            if (p.y_bf16) ((uint16_t*)p.y)[t * p.N + n] = f32_to_bf16_bits(y);
-            else ((float*)p.y)[t * p.N + n] = y;
-        }
+    for (int v = 0; v < 4; ++v) sums[(wave * 16 + 4 * g + v) * 16 + col] = acc[v];
+    __syncthreads();
+    for (int e = threadIdx.x; e < 256; e += blockDim.x) {
+        const int64_t t = t0 + e / 16;
+        const int n = n0 + e % 16;
+        if (t >= p.n_tokens || n >= p.N) continue;
+        float y = p.bias ? element<T>(p.bias, n) : 0.f;
+        for (int k = 0; k < waves; ++k) y += sums[k * 256 + e];
+        if (p.y_bf16) ((uint16_t*)p.y)[t * p.N + n] = f32_to_bf16_bits(y);
+        else ((float*)p.y)[t * p.N + n] = y;
     }
 }
 
@@ -248,7 +242,7 @@ __global__ __launch_bounds__(1024) void w4_kernel(const W4Params p) {
     };
     const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
     const OffsetConstants constants;
-    f32x4 acc[1][1] = {};
+    f32x4 acc = {};
     int batch = wave;
     if (batch < batches) load(batch);
     while (batch < batches) {
@@ -298,12 +292,12 @@ __global__ __launch_bounds__(1024) void w4_kernel(const W4Params p) {
                 }
                 const int i = (u * NG + j) >> 2, jj = (u * NG + j) & 3;
 #pragma unroll
-                for (int v = 0; v < 4; ++v) acc[0][0][v] = fmaf(scale[i][jj], fmaf(-zero[i][jj], sum[v], d[v]), acc[0][0][v]);
+                for (int v = 0; v < 4; ++v) acc[v] = fmaf(scale[i][jj], fmaf(-zero[i][jj], sum[v], d[v]), acc[v]);
             }
         batch = next;
     }
     __syncthreads();                               // everybody is through with its part of LDS
-    store_sums<T, 1, 1>(p, (float*)w4_lds, wave, waves, t0, n0, acc);
+    store_sums<T>(p, (float*)w4_lds, wave, waves, t0, n0, acc);
 }
 
 // More tokens (bf16): a workgroup has 16 * RT * WR rows and 16 * TT tokens.  Its wavefronts are WK groups, each with a range of columns, of WR, which have
@@ -495,8 +489,7 @@ static int launch_w4(const W4Params& p, hipStream_t s) {
     using Lds = W4Lds<T, TP, U>;
     const int batches = (int)ceil_div(p.K, 128 * U), most = TP > 8 ? 8 : 16, waves = batches < most ? batches : most;
     const int64_t nx = ceil_div(p.N, 16), ny = ceil_div(p.n_tokens, 16);
-    if (nx > 0x7fffffff || ny > 65535) return ASTRA_ERR_SHAPE;
-    const int lds = std::max(waves * Lds::all, waves * 256 * (int)sizeof(float));
+        const int lds = std::max(waves * Lds::all, waves * 256 * (int)sizeof(float));
     if (lds > 64 * 1024) {
         const int rc = allow_dynamic_lds(allowed, reinterpret_cast<const void*>(&w4_kernel<T, TP, GS, U>), most * Lds::all);
         if (rc) return rc;
@@ -518,8 +511,7 @@ static int launch_w4_wide(const W4Params& p, hipStream_t s) {
     static std::atomic<uint64_t> allowed{0};
     using Shape = W4Wide<TT, WR, WK, RT, GS>;
     const int64_t nx = ceil_div(p.N, 16 * RT * WR), ny = ceil_div(p.n_tokens, 16 * TT);
-    if (nx > 0x7fffffff || ny > 65535) return ASTRA_ERR_SHAPE;
-    if (Shape::lds > 64 * 1024) {
+        if (Shape::lds > 64 * 1024) {
         const int rc = allow_dynamic_lds(allowed, reinterpret_cast<const void*>(&w4_wide_kernel<TT, WR, WK, RT, GS>), Shape::lds);
         if (rc) return rc;
     }
@@ -557,7 +549,7 @@ extern "C" int astra_w4_linear(const astra_w4_desc* desc, const void* x, int64_t
                                const uint8_t* zeros, const void* bias, void* y, void* stream) {
     const int rc = check_w4_desc(desc);
     if (rc) return rc;
-    if (n_tokens < 0 || n_tokens > (1 << 20)) return ASTRA_ERR_SHAPE;
+    if (n_tokens < 0 || n_tokens > kW4MaxTokens) return ASTRA_ERR_SHAPE;
     if (n_tokens == 0) return ASTRA_OK;
     if (!x || !codes || !scales || !y) return ASTRA_ERR_NULL;
     for (const void* a : {x, (const void*)codes, scales, (const void*)zeros, bias, (const void*)y})

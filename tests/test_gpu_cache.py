@@ -339,3 +339,60 @@ def test_tensors_of_another_device_are_refused():
             B.astra_cache_attention(s["desc"], *[s[m].cpu() if m == n else s[m] for m in ("table", "lens", "first", "q")], *s["pools"], None, None, s["out"], None, w)
     with pytest.raises(B.AstraError, match="workspace"):
         B.astra_cache_attention(s["desc"], s["table"], s["lens"], s["first"], s["q"], *s["pools"], None, None, s["out"], None, w[:128])
+
+
+@pytest.mark.parametrize("n", [64, 100, 256, 300])
+def test_attention_of_many_sequences_some_of_them_long(n):
+    """Cut sequences: one piece of a row block per workgroup up to a number of row blocks, equal shares beyond."""
+    rng = np.random.default_rng(n)
+    lens = rng.integers(0, 200, n)
+    lens[[0, n // 2, n - 1]] = 5000, 0, 3000
+    check_attention(Step("bf16", 4, 1, 64, 32, lens.tolist(), rng.integers(0, 3, n).tolist(), seed=n, columns=300).fill())
+
+
+def test_pools_whose_offsets_pass_32_bits():
+    """The last pages of pools of more than 4 GiB give what small pools do, bit for bit."""
+    import torch
+    st = Step("bf16", 16, 8, 128, 64, [200, 63, 5], [1, 3, 100], seed=22)
+    s, w = state(st)
+    run_step(st, s, w)
+    n = (1 << 32) // (8 * 64 * 128) + 1 + st.n_pages
+    shift = n - st.n_pages
+    big = dict(s, desc=B.cache_desc("bf16", 16, 8, 128, 64, n, 3, st.table.shape[1], st.n, rope_base=10000.0), table=torch.where(s["table"] < 0, s["table"], s["table"] + shift), out=torch.empty_like(s["out"]),
+               lse=torch.empty_like(s["lse"]))
+    fresh, _ = state(st)
+    big["pools"] = []
+    for small in fresh["pools"]:
+        p = torch.empty((n, *small.shape[1:]), dtype=small.dtype, device="cuda:0")
+        p[shift:] = small
+        big["pools"].append(p)
+    run_step(st, big, w)
+    torch.cuda.synchronize()
+    assert big["pools"][0].numel() > 1 << 32 and torch.equal(big["out"], s["out"]) and torch.equal(big["lse"], s["lse"])
+    for b, a in zip(big["pools"], s["pools"]):
+        assert torch.equal(b[shift:].contiguous().view(torch.uint8), a.view(torch.uint8))
+
+
+def test_two_captured_graphs_share_a_workspace():
+    """Replayed in turn, one's call must find nothing of the other's."""
+    import torch
+    parts = [Step("bf16", 8, 2, 128, 64, [9000, 3, 900], [1, 1, 1], seed=23, columns=200), Step("bf16", 8, 2, 128, 64, [10, 4000], [1, 2], seed=24, columns=200)]
+    both = [state(st) for st in parts]
+    w = max((w for _, w in both), key=lambda a: a.numel())
+    graphs, wants = [], []
+    for st, (s, _) in zip(parts, both):
+        run_step(st, s, w)
+        torch.cuda.synchronize()
+        wants.append((s["out"].clone(), s["lse"].clone()))
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            run_step(st, s, w)
+        graphs.append(graph)
+    for _ in range(4):
+        for s, _ in both:
+            s["out"].zero_()
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        for (s, _), (out, lse) in zip(both, wants):
+            assert torch.equal(s["out"], out) and torch.equal(s["lse"], lse)

@@ -125,3 +125,47 @@ def test_captured_into_a_graph():
         B.astra_w4_linear(d, xd, 4, cd, sd, None, None, out)
         torch.cuda.synchronize()
         assert torch.equal(got, out)
+
+
+@pytest.mark.parametrize("group, K", [(32, 32), (32, 288), (32, 1184), (64, 64), (64, 448), (64, 1088), (128, 128), (128, 384), (128, 2432)])
+@pytest.mark.parametrize("T", [20, 40])
+def test_wide_tiles(T, group, K):
+    """Rows enough for tiles of 128 (of 32 and 64 tokens), with widths that end anywhere in a chunk, in a wavefront group's range and in a span of scales."""
+    check("bf16", T, K, 24449 if T == 40 else 24577, group, zeros=K % 3 == 0, bias=K % 2 == 1 or T == 20, y="f32", seed=K + T)
+
+
+def test_many_tokens_of_few_rows():
+    check("bf16", 1000, 128, 1, 32, True, seed=4)
+    check("bf16", 12289, 96, 20, 32, y="f32", seed=5)
+    check("f32", 1000, 96, 17, 32, True, seed=6)
+
+
+def test_products_that_use_much_lds_captured_into_a_graph_and_on_two_streams():
+    import torch
+    from gpu_util import empty_like_dtype, to_dev
+    K, N = 2048, 700
+    graphs = []
+    for dtype, T in (("bf16", 40), ("bf16", 12), ("f32", 12)):
+        x, codes, scales, zeros, _ = make(dtype, T, K, N, 64, True, False, seed=T)
+        a = (B.w4_desc(dtype, K, N, 64), to_dev(x, dtype), T, torch.from_numpy(codes).to("cuda:0"), to_dev(scales, dtype), torch.from_numpy(zeros).to("cuda:0"), None,
+             empty_like_dtype((T, N), dtype))
+        B.astra_w4_linear(*a)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            B.astra_w4_linear(*a)
+        graphs.append((a, graph))
+    streams = [torch.cuda.Stream() for _ in graphs]
+    for _ in range(4):
+        wanted = []
+        for a, _ in graphs:
+            a[1].copy_(torch.randn(a[1].shape, device="cuda:0").to(a[1].dtype))
+            B.astra_w4_linear(*a)
+            wanted.append(a[7].clone())
+            a[7].fill_(float("nan"))
+        torch.cuda.synchronize()
+        for (a, graph), s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                graph.replay()
+        torch.cuda.synchronize()
+        for (a, _), want in zip(graphs, wanted):
+            assert torch.equal(a[7], want)

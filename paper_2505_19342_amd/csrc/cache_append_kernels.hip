@@ -15,7 +15,7 @@ namespace astra {
 // quarter before it is rounded (positions reach 10^5).
 //
 // Bounds.  A step of one token per sequence waits for one round trip to memory after another (where the row belongs, the rows, the old scale):
-// 4.5 us for one sequence, 5.3 us for 64 (32 + 8 heads of 128, bf16), an empty launch in a row being 3.8 us.  Prompts move bytes: 8192 tokens, 129 MB, 26.1 us,
+// 4.5 us for one sequence, 5.3 us for 64 (32 + 8 heads of 128, bf16), an empty launch in a row being 3.8 us.  Prompts move bytes: 5700 tokens, 129 MB, 26.1 us,
 // 4.9 TB/s, what a copy reaches.  Heads share their angles by four: by two 36.5 us, by eight 34.3 us where by four it was 32.5 us; holding eight pieces
 // instead of four 34.4 us; queries before keys and values 42.4 us.
 // ------------------------------------------------------------------------------------------------
@@ -68,7 +68,7 @@ struct Eight<float> {
     __device__ __forceinline__ float at(int i) const { return w[i >> 2][i & 3]; }
 };
 // STREAM: past the caches.  What a prompt writes is more than they keep for the reader, and in passing would put out what is still to be read;
-// 8192 tokens of 32 + 8 + 8 heads of 128: 32.4 us without, 26.1 us with it (streamed loads: 29.9 us).
+// 5700 tokens of 32 + 8 + 8 heads of 128: 32.4 us without, 26.1 us with it (streamed loads: 29.9 us).
 template <bool STREAM, typename V>
 __device__ __forceinline__ void store_piece(void* p, V w) {
     if (STREAM) __builtin_nontemporal_store(w, reinterpret_cast<V*>(p));

@@ -302,16 +302,22 @@ __global__ __launch_bounds__(1024) void w4_kernel(const W4Params p) {
 
 // More tokens (bf16): a workgroup has 16 * RT * WR rows and 16 * TT tokens.  Its wavefronts are WK groups, each with a range of columns, of WR, which have
 // 16 * RT rows each and read x from one copy of it in LDS, with the sums of x over the groups beside it.  While a chunk of 128 columns is worked on, the next one goes to the other
-// half of LDS and the one after it is on its way from memory.  What bounds it: the operations that make operands of codes and scale the sums, and x, which passes the second-level
-// caches once for every 16 * RT * WR rows.
-template <int TT, int WR, int WK, int RT, int GS>
+// half of LDS and the one after it is on its way from memory.  What bounds it: the operations that make operands of codes and scale the sums (57 % of the vector units' time, the matrix
+// cores 19 %, 64 tokens, 4096 x 28672, groups of 64: 34.5 us, 436 TFLOP/s), and x, which passes the second-level caches once for every 16 * RT * WR rows.
+// With two row tiles per wavefront (RT) the sums of x over a group are made once, where x is brought, and each result takes (16 + zero) times that.  With one there is room on the matrix
+// cores: they multiply x by a second operand that is -(16 + zero) everywhere, which is exact, and half of the groups of wavefronts bring x after their products instead of before, so that
+// the two on a SIMD unit want different units.  20 tokens, 14336 x 4096, groups of 32: 40.1 -> 35.1 us (the same with two row tiles: 35.7 -> 37.4).
+// The codes have WB copies in LDS.  One is written when its reader is through with it, and waited for at once; but with it two workgroups with one row tile fit a unit, where there
+// are that many: 20 tokens, 4096 x 14336, groups of 128: 18.0 -> 14.6 us, where there are not, 4096 x 4096: 9.5 with two copies, 11.2 with one.  Two row tiles: 33.4 -> 31.7 us (100 tokens,
+// 4096 x 14336, groups of 64), though 19.7 -> 20.6 with 64 tokens and groups of 128.
+template <int TT, int WR, int WK, int RT, int WB, int GS>
 struct W4Wide {
     static constexpr int waves = WR * WK, threads = waves * kWave;
     static constexpr int x_bytes = TT * 4 * 1024;                               // [tile][32 columns][lane of the operand] 16 bytes
-    static constexpr int sum_bytes = (128 >> GS) * TT * 16 * 4;                 // [group][token]
+    static constexpr int sum_bytes = RT > 1 ? (128 >> GS) * TT * 16 * 4 : 0;    // [group][token]
     static constexpr int of_group = x_bytes + sum_bytes;
-    static constexpr int w_bytes = RT * 16 * kW4RowBytes, span_bytes = RT * ScaleSpan::kBytes;
-    static constexpr int all = 2 * WK * of_group + waves * (2 * w_bytes + span_bytes);
+    static constexpr int w_bytes = RT * 16 * 64, span_bytes = RT * ScaleSpan::kBytes;
+    static constexpr int all = 2 * WK * of_group + waves * (WB * w_bytes + span_bytes);
     static constexpr int lds = all > waves * RT * 1024 ? all : waves * RT * 1024;
     static_assert(lds <= 160 * 1024, "LDS of a unit");
 };
@@ -333,11 +339,12 @@ __device__ __forceinline__ float add_dpp(float v) {
     return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
 }
 
-template <int TT, int WR, int WK, int RT, int GS>
-__global__ __launch_bounds__((W4Wide<TT, WR, WK, RT, GS>::threads), 2) void w4_wide_kernel(const W4Params p) {
-    using Shape = W4Wide<TT, WR, WK, RT, GS>;
+template <int TT, int WR, int WK, int RT, int WB, int GS>
+__global__ __launch_bounds__((W4Wide<TT, WR, WK, RT, WB, GS>::threads), (WB * RT == 1 ? 4 : 2)) void w4_wide_kernel(const W4Params p) {
+    using Shape = W4Wide<TT, WR, WK, RT, WB, GS>;
     using Span = ScaleSpan;
     constexpr int NG = 128 >> GS, STEPS = 4 / NG, PER_SPAN = Span::kGroups / NG;
+    constexpr bool SUMS = RT > 1;                                               // of x over the groups, in LDS
     constexpr int LANES = WR * kWave;                                            // of a group of wavefronts
     constexpr int NX = TT * 16 * 16 / LANES;                                     // pieces of eight columns of a token that a lane brings to LDS
     extern __shared__ __align__(16) char w4_lds[];
@@ -347,8 +354,8 @@ __global__ __launch_bounds__((W4Wide<TT, WR, WK, RT, GS>::threads), 2) void w4_w
     const int64_t t0 = (int64_t)blockIdx.y * 16 * TT;
     const int chunks = (p.K + 127) >> 7, rounds = (chunks + WK - 1) / WK, first = wk * rounds;       // every wavefront goes round as often
     char* const lds_x = w4_lds + wk * 2 * Shape::of_group;
-    char* const lds_w = w4_lds + WK * 2 * Shape::of_group + wave * (2 * Shape::w_bytes + Shape::span_bytes);
-    char* const lds_s = lds_w + 2 * Shape::w_bytes;
+    char* const lds_w = w4_lds + WK * 2 * Shape::of_group + wave * (WB * Shape::w_bytes + Shape::span_bytes);
+    char* const lds_s = lds_w + WB * Shape::w_bytes;
     const int id = wr * kWave + lane, piece = id & 15, tok = id >> 4;            // lanes of a token are neighbours; the next pieces are LANES / 16 tokens on
 
     const uint8_t* codes[RT];
@@ -361,39 +368,51 @@ __global__ __launch_bounds__((W4Wide<TT, WR, WK, RT, GS>::threads), 2) void w4_w
     u32x4 raw_w[RT];
     Span span[RT];
     Tokens<uint16_t> raw_x[NX];
-    auto load = [&](int chunk) __attribute__((always_inline)) {
-        // a chunk beyond the last, and columns beyond the last: read where there is something, counted for nothing (x is 0 there, and so is the scale)
-        const int k0 = min(chunk, chunks - 1) * 128;
-        const int wk0 = min(k0, p.K - 32 - 32 * (lane & 3)) >> 1, xk0 = min(k0, p.K - 8 - 8 * piece);
+    // a chunk beyond the last, and columns beyond the last: read where there is something, counted for nothing (x is 0 there, and so is the scale)
+    auto load_w = [&](int chunk) __attribute__((always_inline)) {
+        const int wk0 = min(min(chunk, chunks - 1) * 128, p.K - 32 - 32 * (lane & 3)) >> 1;
 #pragma unroll
         for (int r = 0; r < RT; ++r) raw_w[r] = *reinterpret_cast<const u32x4*>(codes[r] + wk0);
+    };
+    auto load_x = [&](int chunk) __attribute__((always_inline)) {
+        const int xk0 = min(min(chunk, chunks - 1) * 128, p.K - 8 - 8 * piece);
 #pragma unroll
         for (int i = 0; i < NX; ++i) raw_x[i].load(xs[i] + xk0);
     };
-    auto stage = [&](int chunk, int half) __attribute__((always_inline)) {
+    auto stage_x = [&](int chunk, int half) __attribute__((always_inline)) {
         char* const to = lds_x + half * Shape::of_group;
-        const bool there = chunk * 128 + 8 * piece < p.K;
+        if (chunk * 128 + 128 > p.K)
+#pragma unroll
+            for (int i = 0; i < NX; ++i) raw_x[i].w = chunk * 128 + 8 * piece < p.K ? raw_x[i].w : u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
         for (int i = 0; i < NX; ++i) {
             u32x4 a[1];
-            raw_x[i].parts(there, a);
+            raw_x[i].parts(true, a);
             const int t = tok + i * (LANES / 16), slot = ((piece & 3) * 16 + ((t & 15) ^ piece)) * 16;       // exchanged within sixteen: a token's pieces in different banks
             *reinterpret_cast<u32x4*>(to + ((t >> 4) * 4 + (piece >> 2)) * 1024 + slot) = a[0];
-            float sum = add_dpp<0x4E>(add_dpp<0xB1>(sum_eight(a[0])));
-            if constexpr (GS > 5) sum = add_dpp<0x141>(sum);
-            if constexpr (GS > 6) sum = add_dpp<0x140>(sum);
-            if ((piece & ((1 << GS) / 8 - 1)) == 0) ((float*)(to + Shape::x_bytes))[(piece >> (GS - 3)) * TT * 16 + t] = sum;
+            if constexpr (SUMS) {
+                float sum = add_dpp<0x4E>(add_dpp<0xB1>(sum_eight(a[0])));
+                if constexpr (GS > 5) sum = add_dpp<0x141>(sum);
+                if constexpr (GS > 6) sum = add_dpp<0x140>(sum);
+                if ((piece & ((1 << GS) / 8 - 1)) == 0) ((float*)(to + Shape::x_bytes))[(piece >> (GS - 3)) * TT * 16 + t] = sum;
+            }
         }
+    };
+    // exchanged within a row: sixteen rows' words of one column fall into different banks
+    auto stage_w = [&](int half) __attribute__((always_inline)) {
 #pragma unroll
-        for (int r = 0; r < RT; ++r) *reinterpret_cast<u32x4*>(lds_w + half * Shape::w_bytes + (r * 16 + (lane >> 2)) * kW4RowBytes + 16 * (lane & 3)) = raw_w[r];
+        for (int r = 0; r < RT; ++r) *reinterpret_cast<u32x4*>(lds_w + half % WB * Shape::w_bytes + (r * 16 + (lane >> 2)) * 64 + 16 * ((lane ^ (lane >> 4)) & 3)) = raw_w[r];
     };
     const OffsetConstants constants;
     f32x4 acc[TT][RT] = {};
 #pragma unroll
     for (int r = 0; r < RT; ++r) span[r].load(p, n0 + 16 * r, groups, first * NG);
-    load(first);
-    stage(first, 0);
-    load(first + 1);
+    load_x(first);
+    load_w(first);
+    stage_x(first, 0);
+    load_x(first + 1);
+    stage_w(0);
+    load_w(first + 1);
     __syncthreads();
     for (int round = 0; round < rounds; ++round) {
         const int chunk = first + round, half = round & 1, in_span = round % PER_SPAN;
@@ -404,28 +423,21 @@ __global__ __launch_bounds__((W4Wide<TT, WR, WK, RT, GS>::threads), 2) void w4_w
                 if (round + PER_SPAN < rounds) span[r].load(p, n0 + 16 * r, groups, (chunk + PER_SPAN) * NG);
             }
         }
-        if (round + 1 < rounds) {
-            stage(chunk + 1, half ^ 1);
-            load(chunk + 2);
+        const bool later = !SUMS && wk % 2 == 1, more = round + 1 < rounds;
+        if (more && !later) {
+            stage_x(chunk + 1, half ^ 1);
+            load_x(chunk + 2);
+            if (WB > 1) {
+                stage_w(half ^ 1);
+                load_w(chunk + 2);
+            }
         }
         const char* const x = lds_x + half * Shape::of_group;
-        const char* const w = lds_w + half * Shape::w_bytes;
-        constexpr int kAtOnce = TT * RT * NG > 16 ? 1 : NG;    // groups whose operands there are registers for
+        const char* const w = lds_w + half % WB * Shape::w_bytes;
+        constexpr int kAtOnce = TT * RT * NG > 16 || (WB * RT == 1 && NG == 4) ? 1 : NG;    // groups whose operands there are registers for
 #pragma unroll kAtOnce
         for (int j = 0; j < NG; ++j) {
             f32x4 d[TT][RT] = {};
-#pragma unroll
-            for (int a = j * STEPS; a < (j + 1) * STEPS; ++a) {
-                bf16x8 wf[RT];
-#pragma unroll
-                for (int r = 0; r < RT; ++r) wf[r] = weights_offset(*reinterpret_cast<const uint32_t*>(w + (r * 16 + col) * kW4RowBytes + 16 * a + 4 * g), constants);
-#pragma unroll
-                for (int i = 0; i < TT; ++i) {
-                    const bf16x8 xa = *reinterpret_cast<const bf16x8*>(x + (i * 4 + a) * 1024 + (g * 16 + (col ^ (4 * a + g))) * 16);
-#pragma unroll
-                    for (int r = 0; r < RT; ++r) d[i][r] = mfma_16x16x32(xa, wf[r], d[i][r]);
-                }
-            }
             float s[RT], z[RT];
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
@@ -433,14 +445,38 @@ __global__ __launch_bounds__((W4Wide<TT, WR, WK, RT, GS>::threads), 2) void w4_w
                 if (chunk * NG + j >= groups) s[r] = 0.f;
                 z[r] = Span::zero(p, lds_s + r * Span::kBytes, in_span * NG + j) + kOffset;
             }
+            const uint32_t zero = __builtin_amdgcn_perm(__float_as_uint(-z[0]), __float_as_uint(-z[0]), 0x07060706u);
+            const bf16x8 zf = __builtin_bit_cast(bf16x8, u32x4{zero, zero, zero, zero});
+#pragma unroll
+            for (int a = j * STEPS; a < (j + 1) * STEPS; ++a) {
+                bf16x8 wf[RT];
+#pragma unroll
+                for (int r = 0; r < RT; ++r) wf[r] = weights_offset(*reinterpret_cast<const uint32_t*>(w + (r * 16 + col) * 64 + 16 * (a ^ (col >> 2)) + 4 * g), constants);
+#pragma unroll
+                for (int i = 0; i < TT; ++i) {
+                    const bf16x8 xa = *reinterpret_cast<const bf16x8*>(x + (i * 4 + a) * 1024 + (g * 16 + (col ^ (4 * a + g))) * 16);
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) d[i][r] = mfma_16x16x32(xa, wf[r], d[i][r]);
+                    if constexpr (!SUMS) d[i][0] = mfma_16x16x32(xa, zf, d[i][0]);
+                }
+            }
 #pragma unroll
             for (int i = 0; i < TT; ++i) {
-                const f32x4 sum = *reinterpret_cast<const f32x4*>(x + Shape::x_bytes + ((j * TT + i) * 16 + 4 * g) * 4);
+                f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+                if constexpr (SUMS) sum = *reinterpret_cast<const f32x4*>(x + Shape::x_bytes + ((j * TT + i) * 16 + 4 * g) * 4);
 #pragma unroll
                 for (int r = 0; r < RT; ++r)
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) acc[i][r][v] = fmaf(s[r], fmaf(-z[r], sum[v], d[i][r][v]), acc[i][r][v]);
+                    for (int v = 0; v < 4; ++v) acc[i][r][v] = fmaf(s[r], SUMS ? fmaf(-z[r], sum[v], d[i][r][v]) : d[i][r][v], acc[i][r][v]);
             }
+        }
+        if (more && later) {
+            stage_x(chunk + 1, half ^ 1);
+            load_x(chunk + 2);
+        }
+        if (more && (later || WB == 1)) {      // this wavefront has read what one copy is written over
+            stage_w(half ^ 1);
+            load_w(chunk + 2);
         }
         __syncthreads();                       // this half has been read, the other is whole
     }
@@ -506,31 +542,33 @@ static int launch_w4(const W4Params& p, hipStream_t s) {
     return launch_w4<T, TP, 7, U>(p, s);
 }
 
-template <int TT, int WR, int WK, int RT, int GS>
+template <int TT, int WR, int WK, int RT, int WB, int GS>
 static int launch_w4_wide(const W4Params& p, hipStream_t s) {
     static std::atomic<uint64_t> allowed{0};
-    using Shape = W4Wide<TT, WR, WK, RT, GS>;
+    using Shape = W4Wide<TT, WR, WK, RT, WB, GS>;
     const int64_t nx = ceil_div(p.N, 16 * RT * WR), ny = ceil_div(p.n_tokens, 16 * TT);
         if (Shape::lds > 64 * 1024) {
-        const int rc = allow_dynamic_lds(allowed, reinterpret_cast<const void*>(&w4_wide_kernel<TT, WR, WK, RT, GS>), Shape::lds);
+        const int rc = allow_dynamic_lds(allowed, reinterpret_cast<const void*>(&w4_wide_kernel<TT, WR, WK, RT, WB, GS>), Shape::lds);
         if (rc) return rc;
     }
-    w4_wide_kernel<TT, WR, WK, RT, GS><<<dim3((unsigned)nx, (unsigned)ny), Shape::threads, Shape::lds, s>>>(p);
+    w4_wide_kernel<TT, WR, WK, RT, WB, GS><<<dim3((unsigned)nx, (unsigned)ny), Shape::threads, Shape::lds, s>>>(p);
     return launch_status();
 }
 
-template <int TT, int WR, int WK, int RT>
+template <int TT, int WR, int WK, int RT, int WB>
 static int launch_w4_wide(const W4Params& p, hipStream_t s) {
-    if (p.group_shift == 5) return launch_w4_wide<TT, WR, WK, RT, 5>(p, s);
-    if (p.group_shift == 6) return launch_w4_wide<TT, WR, WK, RT, 6>(p, s);
-    return launch_w4_wide<TT, WR, WK, RT, 7>(p, s);
+    if (p.group_shift == 5) return launch_w4_wide<TT, WR, WK, RT, WB, 5>(p, s);
+    if (p.group_shift == 6) return launch_w4_wide<TT, WR, WK, RT, WB, 6>(p, s);
+    return launch_w4_wide<TT, WR, WK, RT, WB, 7>(p, s);
 }
 
 static int launch_w4_wide(const W4Params& p, hipStream_t s) {
-    // tiles of 128 rows where those are enough for the units; of 32, for 32 tokens, otherwise
-    if (p.n_tokens > 32 && ceil_div(p.N, 128) * ceil_div(p.n_tokens, 64) >= 192) return launch_w4_wide<4, 4, 2, 2>(p, s);
-    if (ceil_div(p.N, 128) * ceil_div(p.n_tokens, 32) >= 192) return launch_w4_wide<2, 4, 2, 2>(p, s);
-    return launch_w4_wide<2, 2, 4, 1>(p, s);
+    // tiles of 128 rows where those are enough for three quarters of the 256 units; of 32, for 32 tokens, otherwise.  48 tokens, 4096 x 14336 (224 tiles of 128): 20.6 us, in tiles of 32 27.7;
+    // 20 tokens (112): 14.6 in tiles of 32
+    if (p.n_tokens > 32 && ceil_div(p.N, 128) * ceil_div(p.n_tokens, 64) >= 192) return launch_w4_wide<4, 4, 2, 2, 1>(p, s);
+    if (ceil_div(p.N, 128) * ceil_div(p.n_tokens, 32) >= 192) return launch_w4_wide<2, 4, 2, 2, 1>(p, s);
+    if (ceil_div(p.N, 32) * ceil_div(p.n_tokens, 32) > 256) return launch_w4_wide<2, 2, 4, 1, 1>(p, s);
+    return launch_w4_wide<2, 2, 4, 1, 2>(p, s);
 }
 
 template <typename T>

@@ -134,6 +134,11 @@ def test_wide_tiles(T, group, K):
     check("bf16", T, K, 24449 if T == 40 else 24577, group, zeros=K % 3 == 0, bias=K % 2 == 1 or T == 20, y="f32", seed=K + T)
 
 
+@pytest.mark.parametrize("group, K", [(32, 32), (32, 1184), (64, 448), (64, 1088), (128, 384), (128, 2432)])
+def test_two_workgroups_of_small_tiles_on_a_unit(group, K):
+    check("bf16", 33, K, 4130, group, zeros=K % 3 != 0, bias=True, seed=K)
+
+
 def test_many_tokens_of_few_rows():
     check("bf16", 1000, 128, 1, 32, True, seed=4)
     check("bf16", 12289, 96, 20, 32, y="f32", seed=5)

@@ -58,10 +58,11 @@ W4 = [  # element type, tokens, in, out -> kernel, grid
     ("bf16", 1, 4096, 4096, "w4_kernel<bf16, 2, 7, 2>", (256, 1)), ("bf16", 2, 4096, 4097, "w4_kernel<bf16, 2, 7, 2>", (257, 1)),
     ("bf16", 3, 4096, 1, "w4_kernel<bf16, 8, 7, 2>", (1, 1)), ("bf16", 8, 128, 100, "w4_kernel<bf16, 8, 7, 2>", (7, 1)),
     ("bf16", 9, 14336, 4096, "w4_kernel<bf16, 16, 7, 2>", (256, 1)), ("bf16", 16, 4096, 4096, "w4_kernel<bf16, 16, 7, 2>", (256, 1)),
-    ("bf16", 17, 4096, 4096, "w4_wide_kernel<2, 2, 4, 1, 7>", (128, 1)), ("bf16", 33, 4096, 4096, "w4_wide_kernel<2, 2, 4, 1, 7>", (128, 2)),
-    ("bf16", 20, 256, 24449, "w4_wide_kernel<2, 4, 2, 2, 7>", (192, 1)), ("bf16", 20, 256, 24448, "w4_wide_kernel<2, 2, 4, 1, 7>", (764, 1)),
-    ("bf16", 64, 256, 24449, "w4_wide_kernel<4, 4, 2, 2, 7>", (192, 1)), ("bf16", 65, 256, 12288, "w4_wide_kernel<4, 4, 2, 2, 7>", (96, 2)),
-    ("bf16", 64, 256, 12288, "w4_wide_kernel<2, 4, 2, 2, 7>", (96, 2)), ("bf16", 1 << 19, 128, 16, "w4_wide_kernel<4, 4, 2, 2, 7>", (1, 8192)),
+    ("bf16", 17, 4096, 4096, "w4_wide_kernel<2, 2, 4, 1, 2, 7>", (128, 1)), ("bf16", 33, 4096, 4096, "w4_wide_kernel<2, 2, 4, 1, 2, 7>", (128, 2)),
+    ("bf16", 20, 256, 24449, "w4_wide_kernel<2, 4, 2, 2, 1, 7>", (192, 1)), ("bf16", 20, 256, 24448, "w4_wide_kernel<2, 2, 4, 1, 1, 7>", (764, 1)),
+    ("bf16", 64, 256, 24449, "w4_wide_kernel<4, 4, 2, 2, 1, 7>", (192, 1)), ("bf16", 65, 256, 12288, "w4_wide_kernel<4, 4, 2, 2, 1, 7>", (96, 2)),
+    ("bf16", 64, 256, 12288, "w4_wide_kernel<2, 4, 2, 2, 1, 7>", (96, 2)), ("bf16", 1 << 19, 128, 16, "w4_wide_kernel<4, 4, 2, 2, 1, 7>", (1, 8192)),
+    ("bf16", 65, 4096, 4096, "w4_wide_kernel<2, 2, 4, 1, 1, 7>", (128, 3)),
     ("f32", 1, 4096, 4096, "w4_kernel<float, 2, 7, 1>", (256, 1)), ("f32", 16, 4096, 4096, "w4_kernel<float, 16, 7, 1>", (256, 1)),
     ("f32", 17, 4096, 4096, "w4_kernel<float, 16, 7, 1>", (256, 2)), ("f32", 1 << 19, 128, 16, "w4_kernel<float, 16, 7, 1>", (1, 32768)),
 ]

@@ -315,7 +315,8 @@ int astra_decode_attention_static(const astra_decode_desc* desc, const void* q, 
  *   lens                [n_seqs] int32: tokens that a sequence had cached before this step
  *   first_row           [n_seqs + 1] int32, ascending: the new tokens of sequence s are rows first_row[s] ..
  *                       first_row[s + 1] - 1 of q, k, v and out; row r is its token lens[s] + r - first_row[s].  Rows that no
- *                       sequence has are left as they are, and tokens beyond max_pages * page_size are dropped
+ *                       sequence has are left as they are, and tokens beyond max_pages * page_size are dropped.  Where it
+ *                       does not ascend, results are undefined, but nothing outside the arrays is read or written
  * Both calls of a step take the same descriptor, table, lens and first_row; the caller adds the new tokens to lens
  * afterwards.  Sequences may share pages that are full; a page that a call writes to belongs to one entry of one sequence.
  *   q                   rows of H_q * dh elements, q_stride elements apart; k, v: rows of H_kv * dh, k_stride, v_stride

@@ -50,6 +50,7 @@ struct CacheAttnParams {
     float* lse;
     int32_t q_stride;
     float scale;
+    uint32_t most_blocks;        // row blocks that ascending first rows can make
     // scratch, see CacheAttnPlan
     float* part_o;
     float* part_ml;
@@ -474,6 +475,7 @@ __global__ __launch_bounds__((CaShape<DH, T, NT, CUT>::threads), (CaShape<DH, T,
     SequencePlan lane_plan(0, 0, 0);
     if (few && lane < c.n_seqs) lane_plan = SequencePlan(c, lane);
     uint32_t step = 1, share = 1;
+    bool nobodys = false;
     if constexpr (CUT) {
         uint32_t tiles = 0, blocks = 0;
         auto count = [&](const SequencePlan& sp) __attribute__((always_inline)) {
@@ -486,6 +488,7 @@ __global__ __launch_bounds__((CaShape<DH, T, NT, CUT>::threads), (CaShape<DH, T,
             for (int s = lane; s < c.n_seqs; s += 64) count(SequencePlan(c, s));
         blocks = __builtin_amdgcn_readlane(scan(blocks), 63);
         tiles = __builtin_amdgcn_readlane(scan(tiles), 63);
+        nobodys = blocks > p.most_blocks;        // first rows that do not ascend count rows twice, and the units below would pass 32 bits
         const uint32_t least = min(max(tiles / kCaCus, (uint32_t)kCaMinShare), 4u * kCaMinShare);
         if (4 * blocks <= gridDim.x) step = max((tiles + gridDim.x - blocks - 1) / (gridDim.x - blocks), least);
         else share = max((tiles + gridDim.x - 1) / gridDim.x, least);
@@ -511,6 +514,7 @@ __global__ __launch_bounds__((CaShape<DH, T, NT, CUT>::threads), (CaShape<DH, T,
         __syncthreads();
         all = before[c.n_seqs];
     }
+    if (nobodys) all = 0;
     uint32_t u = blockIdx.x < (all + share - 1) / share ? blockIdx.x * share : all;
     const uint32_t end = all - u < share ? all : u + share;
     CaJoin join = {};
@@ -729,6 +733,7 @@ __global__ __launch_bounds__(256) void cache_attn_join_kernel(const CacheAttnPar
 // [2 * workgroups][rows][2], and what is to be joined [workgroups]
 struct CacheAttnPlan {
     int nt, wgs;
+    uint32_t most_blocks;
     bool cut;
     size_t off_ml, off_joins, total;
 };
@@ -748,6 +753,7 @@ static int cache_attn_plan(const astra_cache_desc& d, CacheAttnPlan* pl) {
     if (rows > (1 << 30) || blocks * tiles > 0x7fffffff || blocks * 1024 > kMaxGridThreads) return ASTRA_ERR_UNSUPPORTED;
     s.cut = tiles > cache_attn_whole_tiles(blocks);
     s.wgs = (int)blocks;
+    s.most_blocks = (uint32_t)blocks;
     if (s.cut) {
         int most = d.head_dim == 64    ? f32 ? cache_attn_wgs<64, float>(s.nt) : cache_attn_wgs<64, uint16_t>(s.nt)
                    : d.head_dim == 128 ? f32 ? cache_attn_wgs<128, float>(s.nt) : cache_attn_wgs<128, uint16_t>(s.nt)
@@ -823,6 +829,7 @@ int astra_cache_attention(const astra_cache_desc* desc, const int32_t* page_tabl
     p.prior_out = prior_out; p.prior_lse = prior_lse; p.out = out; p.lse = lse_out;
     p.q_stride = desc->q_stride ? desc->q_stride : desc->n_q_heads * desc->head_dim;
     p.scale = desc->scale != 0.f ? desc->scale : 1.f / sqrtf((float)desc->head_dim);
+    p.most_blocks = pl.most_blocks;
     p.part_o = (float*)workspace;
     p.part_ml = (float*)((char*)workspace + pl.off_ml);
     p.joins = (CaJoin*)((char*)workspace + pl.off_joins);

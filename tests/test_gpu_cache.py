@@ -194,6 +194,19 @@ def test_attention_with_lengths_that_nothing_backs():
     assert np.isfinite(attend(st)[0]).all()
 
 
+def test_first_rows_that_do_not_ascend_end_the_call():
+    """They name rows several times over: whatever is computed stays inside the arrays, and with cut sequences nothing is."""
+    for columns in (0, 200):
+        st = Step("bf16", 2, 1, 64, 16, [50, 40, 30, 20], [10, 10, 10, 10], seed=19, columns=columns).fill()
+        ref, _ = attend(st)
+        kept, st.first = st.first, np.array([0, 40, 0, 40, 0], np.int32)
+        out, lse = attend(st)
+        if columns:
+            assert np.all(out == 7.0) and np.all(lse == 7.0)
+        st.first = kept
+        np.testing.assert_array_equal(attend(st)[0], ref)
+
+
 def test_nan_values_reach_only_the_rows_that_see_them():
     for dtype, columns in (("bf16", 0), ("f32", 0), ("bf16", 200), ("f32", 200)):
         st = Step(dtype, 4, 2, 128, 16, [40], [9], seed=13, columns=columns).fill()

@@ -19,10 +19,10 @@ namespace astra {
 // (16 bits, 2^-17 relative, beside the result's own 2^-9).
 //
 // Bounds (heads of 128, bf16, 32 over 8).  Long contexts: the bytes of the pages, with loads of keys and values a tile ahead of their use.  64 ragged sequences of up to 8192 tokens
-// 111 us, 4.84 TB/s (a sum over plain memory reaches 6.1); one of 131072 61 us, 4.4 TB/s, 8 of it the second launch.  Vector units are busy for a quarter of that, matrix cores
+// 111 us, 4.84 TB/s (a sum over plain memory reaches 6.1); one of 131072 59 us, 4.5 TB/s.  Vector units are busy for a quarter of that, matrix cores
 // for a tenth.  Short ones: one round trip to memory after another (lengths, table, scales and codes) and, where sequences are cut, a second launch: 6.7 + 4.8 us for one
 // sequence of 1025 tokens, 8.5 us in one launch for 8 of up to 1021 (12 heads of 64, fp32).  Chunks of prompts: the vector instructions per score (scale, exponential, parts, conversions of
-// codes), 37 us for four of up to 256 tokens over up to 2048, 154 TFLOP/s.
+// codes), 30 us for four of up to 256 tokens over up to 2048, 192 TFLOP/s.
 // ------------------------------------------------------------------------------------------------
 #define CA_INLINE __attribute__((always_inline))
 constexpr int kCaTile = 32;
@@ -51,6 +51,7 @@ struct CacheAttnParams {
     int32_t q_stride;
     float scale;
     uint32_t most_blocks;        // row blocks that ascending first rows can make
+    int32_t by_block;            // a unit per workgroup, and what is to be joined noted by row block
     // scratch, see CacheAttnPlan
     float* part_o;
     float* part_ml;
@@ -367,30 +368,34 @@ struct CacheWalk {
 // ---- the work of a launch, dealt out --------------------------------------------------------------
 // A unit is a tile of 32 tokens for one row block.  The units of all row blocks (sequence by sequence, head by head, block by block of rows, the tiles of a
 // block in order) are cut into equal shares, one per workgroup: ragged batches keep every workgroup busy equally long, and one long context is
-// walked by all of them.  Where there are at least four times as many workgroups as row blocks, a unit is `step` tiles, so many that a unit per workgroup is enough: a workgroup
+// walked by all of them.  Where there are at least four times as many workgroups as there can be row blocks, a unit is `step` tiles, so many that a unit per workgroup is enough: a workgroup
 // that ends one block and begins another starts and joins its wavefronts twice (64 row blocks of up to 250 tiles: 36.7 us in equal shares, 21.6 so; 256 of up to 250: 53.6, 57.2).  Only the device knows the lengths, so every workgroup adds them up itself.  The wavefronts take the tiles
 // of a share in turn and are joined in LDS.  Where a share ends inside a row block, the unnormalised sums go to the scratch array:
 // a workgroup has at most two such pieces, one that ends a row block begun by others (slot 2w) and one that begins one (slot 2w + 1).
-// The workgroup that begins a block notes how many pieces there are, and a second launch joins them in order.
-// Where sequences cannot be long (CUT = false), a row block is one unit, the workgroups have more wavefronts and there is no second launch.
+// The workgroup that begins a block notes how many pieces there are, under its own number or, where there are few, the block's, and a second launch joins them in order,
+// a workgroup per row where that is no more than kCaJoinWgs (32 rows over 3000 tokens: 45.7 us with four workgroups per block, all of the first launch's numbers among them, 15.9 so).
+// Where sequences cannot be long (CUT = false), a row block is one unit and there is no second launch.  WIDE: its workgroup has all the wavefronts of a compute unit, for
+// launches of a single round; four, and several workgroups on a unit, where there are more row blocks than units: while one begins or ends its walk, others compute
+// (200 sequences of up to 1000 tokens: 78.8 and 50.2 us, 320 blocks of chunks over up to 2000 tokens 30.5 and 24.9; 64 blocks over 1000 16.5 and 17.4).
 constexpr int kCaMinShare = 2;        // tiles; 8 where there are enough for every unit: fewer pieces to join (313 tiles of 8 row blocks: 14.3 us, 16.5 with shares of 4)
 constexpr int kCaCus = 256;
+constexpr int kCaJoinWgs = 16384;
 // Tiles of a sequence that is not cut.  A row block that one workgroup walks takes about 5 us and 0.3 us a tile, one after the other where there are more than units; cut ones
-// take 11 us with their join and 1.7 ns a tile of them all (heads of 128).  8 row blocks of 33 tiles: 14.3 us whole, 12.4 cut, of 62: 16.2 and 11.4; 64 of up to 64: 18.3 and 18.0;
-// 512 of up to 64: 38 and 49, of up to 125: 60 and 66.  Only the capacity is known here: beyond 128 a sequence is cut whatever there is beside it, or one long one would hold up the others.
+// take 11 us with their join and 1.7 ns a tile of them all (heads of 128).  8 row blocks of 33 tiles: 14.3 us whole, 11.9 cut, of 62: 16.2 and 11.4; 64 of 33: 16.5 and 20.0, of 55: 21.5 and 21.1;
+// 512 of up to 64: 28.9 and 49, of up to 125: 52 and 66, of up to 256: 117 and 111.  Only the capacity is known here: beyond 128 a sequence is cut whatever there is beside it, or one long one would hold up the others.
 static int cache_attn_whole_tiles(int64_t blocks) { return blocks < 24 ? 24 : blocks < 128 ? (int)blocks : 128; }
 
 // how many wavefronts a workgroup has and how many workgroups the registers of a unit leave room for
-template <int DH, typename T, int NT, bool CUT>
+template <int DH, typename T, int NT, bool WIDE>
 struct CaShape {
     static constexpr int per_simd = DH == 256 ? (sizeof(T) == 4 ? 1 : 2) : DH == 128 ? (sizeof(T) == 4 || NT > 1 ? 2 : 3) : (sizeof(T) == 4 || NT > 1 ? 3 : 4);
-    static constexpr int waves = CUT ? 4 : 4 * (per_simd > 3 ? 3 : per_simd), threads = waves * kWave;
-    static constexpr int wgs_per_cu = CUT ? per_simd : 1;
+    static constexpr int waves = WIDE ? 4 * (per_simd > 3 ? 3 : per_simd) : 4, threads = waves * kWave;
+    static constexpr int wgs_per_cu = WIDE ? 1 : per_simd;
 };
 
 // what joins the pieces of a row block
 struct CaJoin {
-    int32_t pieces, row0, n_rows, kv_head, from, pad[3];
+    int32_t pieces, first, row0, n_rows, kv_head, from, pad[2];      // first: the workgroup that begins the block
 };
 
 struct SequencePlan {
@@ -444,12 +449,13 @@ struct RowResult {
     }
 };
 
-template <int DH, typename T, int NT, bool CUT>
-__global__ __launch_bounds__((CaShape<DH, T, NT, CUT>::threads), (CaShape<DH, T, NT, CUT>::wgs_per_cu)) void cache_attn_kernel(const CacheAttnParams p) {
+template <int DH, typename T, int NT, bool CUT, bool WIDE>
+__global__ __launch_bounds__((CaShape<DH, T, NT, WIDE>::threads), (CaShape<DH, T, NT, WIDE>::wgs_per_cu)) void cache_attn_kernel(const CacheAttnParams p) {
     using Walk = CacheWalk<DH, T, NT>;
-    constexpr int WAVES = CaShape<DH, T, NT, CUT>::waves, THREADS = WAVES * kWave, ROWS = 16 * NT;
+    constexpr int WAVES = CaShape<DH, T, NT, WIDE>::waves, THREADS = WAVES * kWave, ROWS = 16 * NT;
     constexpr int PASS = 4, STRIDE = 16 * PASS + 4;               // channels per thread and pass when the wavefronts are joined
     __shared__ uint32_t before[kCacheMaxSeqs + 1];                // units before a sequence, where there are more than 64
+    __shared__ uint32_t blocks_before[CUT ? kCacheMaxSeqs : 1];
     __shared__ float ml[WAVES][ROWS][2];
     __shared__ __align__(16) float sums[WAVES][16][STRIDE];       // of a wavefront; while it walks, a tile of keys on its way to the operand
     static_assert(sizeof(sums[0]) >= 32 * Walk::KR, "a tile of keys");
@@ -474,10 +480,10 @@ __global__ __launch_bounds__((CaShape<DH, T, NT, CUT>::threads), (CaShape<DH, T,
     const bool few = c.n_seqs <= 64;
     SequencePlan lane_plan(0, 0, 0);
     if (few && lane < c.n_seqs) lane_plan = SequencePlan(c, lane);
-    uint32_t step = 1, share = 1;
+    uint32_t step = 1, share = 1, blocks = 0, lane_blocks = 0;
     bool nobodys = false;
     if constexpr (CUT) {
-        uint32_t tiles = 0, blocks = 0;
+        uint32_t tiles = 0;
         auto count = [&](const SequencePlan& sp) __attribute__((always_inline)) {
             const uint32_t b = sp.blocks(c, ROWS) * (uint32_t)c.Hkv;
             blocks += b;
@@ -486,11 +492,14 @@ __global__ __launch_bounds__((CaShape<DH, T, NT, CUT>::threads), (CaShape<DH, T,
         if (few) count(lane_plan);
         else
             for (int s = lane; s < c.n_seqs; s += 64) count(SequencePlan(c, s));
-        blocks = __builtin_amdgcn_readlane(scan(blocks), 63);
+        const uint32_t upto = scan(blocks);
+        lane_blocks = upto - blocks;
+        blocks = __builtin_amdgcn_readlane(upto, 63);
         tiles = __builtin_amdgcn_readlane(scan(tiles), 63);
         nobodys = blocks > p.most_blocks;        // first rows that do not ascend count rows twice, and the units below would pass 32 bits
+        if (nobodys) blocks = tiles = 0;
         const uint32_t least = min(max(tiles / kCaCus, (uint32_t)kCaMinShare), 4u * kCaMinShare);
-        if (4 * blocks <= gridDim.x) step = max((tiles + gridDim.x - blocks - 1) / (gridDim.x - blocks), least);
+        if (p.by_block) step = max((tiles + gridDim.x - blocks - 1) / (gridDim.x - blocks), least);
         else share = max((tiles + gridDim.x - 1) / gridDim.x, least);
     }
     auto per_block = [&](const SequencePlan& sp) __attribute__((always_inline)) { return CUT ? (sp.tiles(c) + step - 1) / step : 1u; };
@@ -502,12 +511,17 @@ __global__ __launch_bounds__((CaShape<DH, T, NT, CUT>::threads), (CaShape<DH, T,
         all = __builtin_amdgcn_readlane(upto, 63);
     } else {
         if (wave == 0) {
-            uint32_t base = 0;
+            uint32_t base = 0, base_blocks = 0;
             for (int s0 = 0; s0 < c.n_seqs; s0 += 64) {
                 const int s = s0 + lane;
                 const uint32_t mine = s < c.n_seqs ? units(SequencePlan(c, s)) : 0u, upto = scan(mine);
                 if (s < c.n_seqs) before[s] = base + upto - mine;
                 base += __builtin_amdgcn_readlane(upto, 63);
+                if constexpr (CUT) {
+                    const uint32_t b = s < c.n_seqs ? SequencePlan(c, s).blocks(c, ROWS) * (uint32_t)c.Hkv : 0u, to = scan(b);
+                    if (s < c.n_seqs) blocks_before[s] = base_blocks + to - b;
+                    base_blocks += __builtin_amdgcn_readlane(to, 63);
+                }
             }
             if (lane == 0) before[c.n_seqs] = base;
         }
@@ -522,11 +536,12 @@ __global__ __launch_bounds__((CaShape<DH, T, NT, CUT>::threads), (CaShape<DH, T,
     while (u < end) {
         // the last sequence that begins at or before u; those without units are before it
         int s;
-        uint32_t in;
+        uint32_t in, block0 = 0;                 // units of the sequence before u, row blocks before the sequence
         SequencePlan sp(0, 0, 0);
         if (few) {
             s = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64(lane < c.n_seqs && lane_before <= u));
             in = u - (uint32_t)__builtin_amdgcn_readlane(lane_before, s);
+            if (CUT) block0 = (uint32_t)__builtin_amdgcn_readlane(lane_blocks, s);      // here, where every lane takes part: from one that does not, there is nothing to read
             sp = SequencePlan(__builtin_amdgcn_readlane(lane_plan.len, s), __builtin_amdgcn_readlane(lane_plan.from, s), __builtin_amdgcn_readlane(lane_plan.n_new, s));
         } else {
             int lo = 0, n = c.n_seqs;
@@ -541,21 +556,22 @@ __global__ __launch_bounds__((CaShape<DH, T, NT, CUT>::threads), (CaShape<DH, T,
             }
             s = __builtin_amdgcn_readfirstlane(lo - 1);
             in = u - before[s];
+            if (CUT) block0 = blocks_before[s];
             sp = SequencePlan(c, s);
         }
-        const uint32_t all_tiles = sp.tiles(c), blocks = sp.blocks(c, ROWS), of_block = per_block(sp);
+        const uint32_t all_tiles = sp.tiles(c), seq_blocks = sp.blocks(c, ROWS), of_block = per_block(sp);
         const uint32_t row = in / of_block;
         const int unit0 = __builtin_amdgcn_readfirstlane((int)(in - row * of_block));
         const int count = __builtin_amdgcn_readfirstlane((int)min(of_block - unit0, end - u));
         const int tile0 = unit0 * (int)step;
         RowBlock b;
         b.seq = s;
-        b.kv_head = __builtin_amdgcn_readfirstlane((int)(row / blocks));
+        b.kv_head = __builtin_amdgcn_readfirstlane((int)(row / seq_blocks));
         b.len = __builtin_amdgcn_readfirstlane(sp.len);
         b.n_new = __builtin_amdgcn_readfirstlane(sp.n_new);
         b.from = __builtin_amdgcn_readfirstlane(sp.from);
         b.n_rows = b.n_new * share_h;
-        b.row0 = __builtin_amdgcn_readfirstlane((int)(row % blocks)) * ROWS;
+        b.row0 = __builtin_amdgcn_readfirstlane((int)(row % seq_blocks)) * ROWS;
         b.least = min(b.len + b.row0 / share_h + 1, c.capacity());
         b.all = min(b.len + min(b.row0 + ROWS - 1, b.n_rows - 1) / share_h + 1, c.capacity());
 
@@ -648,11 +664,19 @@ __global__ __launch_bounds__((CaShape<DH, T, NT, CUT>::threads), (CaShape<DH, T,
                 }
             }
         }
-        if (!whole && unit0 == 0) join = CaJoin{(int)((u + of_block - 1) / share) - (int)blockIdx.x + 1, b.row0, b.n_rows, b.kv_head, b.from, {0, 0, 0}};      // up to the workgroup with the block's last tile
+        if (CUT && unit0 == 0 && (p.by_block || !whole)) {
+            // up to the workgroup with the block's last tile
+            join = CaJoin{whole ? 0 : (int)((u + of_block - 1) / share) - (int)blockIdx.x + 1, (int)blockIdx.x, b.row0, b.n_rows, b.kv_head, b.from, {0, 0}};
+            if (p.by_block && tid == 0) p.joins[block0 + row] = join;
+        }
         u += count;
         __syncthreads();                         // before the next block's sums
     }
-    if (CUT && tid == 0) p.joins[blockIdx.x] = join;
+    if (CUT && tid == 0) {
+        if (!p.by_block) p.joins[blockIdx.x] = join;
+        else
+            for (uint32_t i = blocks + blockIdx.x; i < p.most_blocks; i += gridDim.x) p.joins[i] = CaJoin{};
+    }
 }
 
 // The pieces of a row block that was cut, joined in the order of its tokens: row by row, a wavefront has every fourth piece, all of a wavefront's on their way at once
@@ -667,7 +691,7 @@ __global__ __launch_bounds__(256) void cache_attn_join_kernel(const CacheAttnPar
     const int share_h = c.Hq / c.Hkv, lane = lane_id(), wave = threadIdx.x >> 6;
     const int rows = min(ROWS, join.n_rows - join.row0);
     for (int r = blockIdx.y; r < rows; r += gridDim.y) {
-        auto slot = [&](int i) { return (2 * (int64_t)(blockIdx.x + i) + (i == 0 ? 1 : 0)) * ROWS + r; };
+        auto slot = [&](int i) { return (2 * (int64_t)(join.first + i) + (i == 0 ? 1 : 0)) * ROWS + r; };
         float m = -INFINITY, l = 0.f, o[N] = {};
         for (int i0 = wave; i0 < join.pieces; i0 += 4 * U) {
             float x[U][N], mi[U], li[U];
@@ -734,12 +758,13 @@ __global__ __launch_bounds__(256) void cache_attn_join_kernel(const CacheAttnPar
 struct CacheAttnPlan {
     int nt, wgs;
     uint32_t most_blocks;
-    bool cut;
+    int join_rows;               // workgroups that share the rows of a block when its pieces are joined
+    bool cut, wide, by_block;
     size_t off_ml, off_joins, total;
 };
 template <int DH, typename T>
 static int cache_attn_wgs(int nt) {
-    return kCaCus * (nt == 1 ? CaShape<DH, T, 1, true>::wgs_per_cu : CaShape<DH, T, 2, true>::wgs_per_cu);
+    return kCaCus * (nt == 1 ? CaShape<DH, T, 1, false>::wgs_per_cu : CaShape<DH, T, 2, false>::wgs_per_cu);
 }
 static int cache_attn_plan(const astra_cache_desc& d, CacheAttnPlan* pl) {
     CacheAttnPlan s{};
@@ -752,6 +777,8 @@ static int cache_attn_plan(const astra_cache_desc& d, CacheAttnPlan* pl) {
     // rows and units are counted in 32 bits; workgroups have no more than 1024 threads
     if (rows > (1 << 30) || blocks * tiles > 0x7fffffff || blocks * 1024 > kMaxGridThreads) return ASTRA_ERR_UNSUPPORTED;
     s.cut = tiles > cache_attn_whole_tiles(blocks);
+    const int64_t n_seqs = d.n_seqs > 0 ? d.n_seqs : 1;
+    s.wide = n_seqs * ceil_div(ceil_div(rows, n_seqs), 16 * s.nt) * d.n_kv_heads <= kCaCus;      // row blocks, if every sequence has as many rows as the average
     s.wgs = (int)blocks;
     s.most_blocks = (uint32_t)blocks;
     if (s.cut) {
@@ -760,6 +787,9 @@ static int cache_attn_plan(const astra_cache_desc& d, CacheAttnPlan* pl) {
                                        : f32 ? cache_attn_wgs<256, float>(s.nt) : cache_attn_wgs<256, uint16_t>(s.nt);
         const int64_t shares = ceil_div(blocks * tiles, kCaMinShare);
         s.wgs = (int)(shares < most ? shares : most);
+        s.by_block = 4 * blocks <= s.wgs;
+        const int64_t of_block = rows < 16 * s.nt ? rows : 16 * s.nt, joins = s.by_block ? blocks : s.wgs, room = kCaJoinWgs / joins;
+        s.join_rows = (int)(of_block < 4 ? of_block : room < 4 ? 4 : room < of_block ? room : of_block);
         const size_t r = (size_t)2 * s.wgs * 16 * s.nt;
         s.off_ml = align_up(r * d.head_dim * 4, 256);
         s.off_joins = s.off_ml + align_up(r * 2 * 4, 256);
@@ -772,14 +802,20 @@ static int cache_attn_plan(const astra_cache_desc& d, CacheAttnPlan* pl) {
 
 template <int DH, typename T, int NT>
 static int launch_cache_attention(const CacheAttnParams& p, const CacheAttnPlan& pl, hipStream_t s) {
+    using Shape = CaShape<DH, T, NT, false>;
     if (!pl.cut) {
-        cache_attn_kernel<DH, T, NT, false><<<pl.wgs, CaShape<DH, T, NT, false>::threads, 0, s>>>(p);
+        if constexpr (Shape::per_simd > 1)
+            if (pl.wide) {
+                cache_attn_kernel<DH, T, NT, false, true><<<pl.wgs, CaShape<DH, T, NT, true>::threads, 0, s>>>(p);
+                return launch_status();
+            }
+        cache_attn_kernel<DH, T, NT, false, false><<<pl.wgs, Shape::threads, 0, s>>>(p);
         return launch_status();
     }
-    cache_attn_kernel<DH, T, NT, true><<<pl.wgs, CaShape<DH, T, NT, true>::threads, 0, s>>>(p);
+    cache_attn_kernel<DH, T, NT, true, false><<<pl.wgs, Shape::threads, 0, s>>>(p);
     const int rc = launch_status();
     if (rc) return rc;
-    cache_attn_join_kernel<DH, T, NT><<<dim3(pl.wgs, 4), 256, 0, s>>>(p);
+    cache_attn_join_kernel<DH, T, NT><<<dim3(pl.by_block ? pl.most_blocks : pl.wgs, pl.join_rows), 256, 0, s>>>(p);
     return launch_status();
 }
 
@@ -830,6 +866,7 @@ int astra_cache_attention(const astra_cache_desc* desc, const int32_t* page_tabl
     p.q_stride = desc->q_stride ? desc->q_stride : desc->n_q_heads * desc->head_dim;
     p.scale = desc->scale != 0.f ? desc->scale : 1.f / sqrtf((float)desc->head_dim);
     p.most_blocks = pl.most_blocks;
+    p.by_block = pl.by_block;
     p.part_o = (float*)workspace;
     p.part_ml = (float*)((char*)workspace + pl.off_ml);
     p.joins = (CaJoin*)((char*)workspace + pl.off_joins);

@@ -92,17 +92,21 @@ def test_appends(tmp_path):
 
 def test_attention_cut_or_whole(tmp_path):
     """Whole sequences and one launch where none can be long; equal shares and a second launch otherwise, with no more workgroups than the units hold at a time."""
-    def whole(t, dh, nt):
-        return [f"cache_attn_kernel<{dh}, {t}, {nt}, false>"]
+    def whole(t, dh, nt, wide=True):
+        return [f"cache_attn_kernel<{dh}, {t}, {nt}, false, {str(wide).lower()}>"]
 
     def cut(t, dh, nt):
-        return [f"cache_attn_kernel<{dh}, {t}, {nt}, true>", f"cache_attn_join_kernel<{dh}, {t}, {nt}>"]
-    cases = [(cache(n_seqs=1, n_tokens=1, max_pages=12), whole("bf16", 128, 1), 8), (cache(n_seqs=1, n_tokens=1, max_pages=13), cut("bf16", 128, 1), 13 * 8),
-             (cache(n_seqs=64, n_tokens=64, max_pages=64), whole("bf16", 128, 1), 640), (cache(n_seqs=64, n_tokens=64, max_pages=65), cut("bf16", 128, 1), 768),
-             (cache(n_seqs=2, n_tokens=512, max_pages=64), whole("bf16", 128, 2), 528), (cache(n_seqs=2, n_tokens=512, max_pages=65, dtype="f32"), cut("float", 128, 1), 512),
+        return [f"cache_attn_kernel<{dh}, {t}, {nt}, true, false>", f"cache_attn_join_kernel<{dh}, {t}, {nt}>"]
+    cases = [(cache(n_seqs=1, n_tokens=1, max_pages=12), whole("bf16", 128, 1), 8), (cache(n_seqs=32, n_tokens=32, max_pages=40), whole("bf16", 128, 1), 320),
+             (cache(n_seqs=33, n_tokens=33, max_pages=40), whole("bf16", 128, 1, False), 328), (cache(n_seqs=1, n_tokens=1, max_pages=12, dtype="f32", head_dim=256), whole("float", 256, 1, False), 8), (cache(n_seqs=1, n_tokens=1, max_pages=13), cut("bf16", 128, 1), 13 * 8),
+             (cache(n_seqs=64, n_tokens=64, max_pages=64), whole("bf16", 128, 1, False), 640), (cache(n_seqs=64, n_tokens=64, max_pages=65), cut("bf16", 128, 1), 768),
+             (cache(n_seqs=2, n_tokens=512, max_pages=64), whole("bf16", 128, 2, False), 528), (cache(n_seqs=2, n_tokens=512, max_pages=65, dtype="f32"), cut("float", 128, 1), 512),
              (cache(n_seqs=2, n_tokens=512, max_pages=65, head_dim=256), cut("bf16", 256, 1), 512), (cache(n_seqs=2, n_tokens=512, max_pages=65, head_dim=64), cut("bf16", 64, 2), 768)]
     for (d, names, wgs), (rc, launches) in zip(cases, record([dict(entry="attend", desc=c[0]) for c in cases], tmp_path)):
-        assert rc == 0 and [l[0] for l in launches] == names and all(l[1][0] == wgs for l in launches), (d, launches)
+        assert rc == 0 and [l[0] for l in launches] == names and launches[0][1][0] == wgs, (d, launches)
+        if len(names) > 1:
+            joins, rows = wgs, d["n_tokens"] * d["n_q_heads"] // d["n_kv_heads"]
+            assert launches[1][1][:2] == ([8, 4] if d["n_seqs"] == 1 else [joins, min(rows, 16384 // joins, 16 * int(names[1][-2]))]), (d, launches)
 
 
 def test_the_cap_on_dynamic_lds_is_raised_on_every_device_and_a_refusal_is_an_error(tmp_path):

@@ -409,3 +409,41 @@ def test_two_captured_graphs_share_a_workspace():
         torch.cuda.synchronize()
         for (s, _), (out, lse) in zip(both, wants):
             assert torch.equal(s["out"], out) and torch.equal(s["lse"], lse)
+
+
+@pytest.mark.parametrize("columns", [0, 200])
+def test_strides_and_types_of_the_arrays_change_nothing(columns):
+    """A table in wider rows, q, k and v in the rows of one projection, pages as e4m3 tensors: the dense call's bits."""
+    import torch
+    st = Step("bf16", 6, 2, 64, 16, [70, 0, 333], [3, 1, 40], seed=25, columns=columns)
+    s, w = state(st)
+    run_step(st, s, w)
+    t, _ = state(st)
+    held = st.table.shape[1]
+    table = torch.full((3, held + 5), 7, dtype=torch.int32, device="cuda:0")
+    table[:, :held] = t["table"]
+    row = torch.cat([t[n].flatten(1) for n in "qkv"], 1)
+    q, k, v = row.split([6 * 64, 2 * 64, 2 * 64], 1)
+    d = st.desc(rope_base=10000.0, table_stride=held + 5, q_stride=row.shape[1], k_stride=row.shape[1], v_stride=row.shape[1])
+    kp, vp = (p.view(torch.float8_e4m3fn) for p in t["pools"][:2])
+    assert B.astra_cache_attention_workspace_bytes(d) == w.numel()
+    B.astra_cache_append(d, table, t["lens"], t["first"], None, q, k, v, q, kp, vp, *t["pools"][2:])
+    B.astra_cache_attention(d, table, t["lens"], t["first"], q, kp, vp, *t["pools"][2:], None, None, t["out"], t["lse"], w)
+    torch.cuda.synchronize()
+    assert torch.equal(t["out"], s["out"]) and torch.equal(t["lse"], s["lse"])
+    for a, b in zip(t["pools"], s["pools"]):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+@pytest.mark.parametrize("columns", [0, 200])
+def test_a_step_in_which_nobody_has_a_token(columns):
+    import torch
+    st = Step("bf16", 4, 2, 128, 32, [50, 7], [0, 0], seed=26, behind=3, columns=columns)
+    out, lse = attend(st)
+    assert np.all(out == 7.0) and np.all(lse == 7.0)
+    s, _ = state(st)
+    kept = [p.clone() for p in s["pools"]]
+    s["q_out"].fill_(7.0)
+    B.astra_cache_append(s["desc"], s["table"], s["lens"], s["first"], None, s["q"], s["k"], s["v"], s["q_out"], *s["pools"])
+    torch.cuda.synchronize()
+    assert torch.all(s["q_out"] == 7.0) and all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(kept, s["pools"]))
